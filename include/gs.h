@@ -330,6 +330,97 @@ typedef struct {
  * GS_ERR_CAPACITY if a tensor has 2^32 elements or more. */
 GsStatus gs_adam_step(GsContext *ctx, const GsAdamTensor *tensors, int32_t num_tensors, int64_t step, void *stream);
 
+/* ---- Beside the scene: the layers of a network over the Gaussians, and the clipping of its gradients -------------
+ * The decoder is fixed and small (App. D varies it between 16 and 32 neurons).  A network of ordinary widths whose
+ * rows are the Gaussians - a trunk that gives the latent features of Eq. 5 from positions or other
+ * latents - is built of the following layers, forward and backward, and trained with the Adam update below.
+ * The paper has no counterpart.
+ *
+ * Rows of activations lie `ld` elements apart (ld >= columns); columns behind the last one are neither read nor written.  No
+ * two arguments of a call overlap, but where it is said.  rows may be 0 and stays below 2^31. */
+typedef enum { GS_TYPE_F32 = 0, GS_TYPE_F16 = 1, GS_TYPE_BF16 = 2 } GsType;
+typedef enum {
+  GS_DENSE_NONE = 0,
+  GS_DENSE_RELU = 1,
+  GS_DENSE_SILU = 2,   /* z / (1 + exp(-z))                                                    */
+  GS_DENSE_GELU = 3    /* tanh form: z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))         */
+} GsDenseActivation;
+enum { GS_DENSE_MAX_FEATURES = 16384, GS_LAYER_NORM_MAX_COLS = 8192, GS_GRAD_MAX_TENSORS = 512, GS_GRAD_MAX_BUFFERS = 1024 };
+
+/* A dense layer's weights (host struct of device pointers).  weight [out_features, in_features], row-major like the decoder's
+ * (out, in), in fp16 or bf16; bias [out_features] fp32, or NULL. */
+typedef struct {
+  const void *weight;
+  int64_t ld_weight;           /* elements from row to row; a multiple of 8                          */
+  const float *bias;
+  int32_t in_features, out_features;   /* 1 .. GS_DENSE_MAX_FEATURES                                 */
+  int32_t dtype;               /* GS_TYPE_F16 or GS_TYPE_BF16: of weight and of all activations      */
+  int32_t activation;          /* GsDenseActivation                                                  */
+} GsDenseLayer;
+
+/* y = act(x W^T + bias) + residual.  x [rows, in_features], y and residual [rows, out_features] in the layer's type, 16-byte
+ * aligned with ld a multiple of 8 (the columns may be any number).  residual may be NULL, or y itself.  preact (may be
+ * NULL) receives x W^T + bias, rounded to the layer's type: what gs_dense_backward wants of a layer with an
+ * activation.  Sums, bias, activation and residual are taken in fp32, y is rounded once. */
+GsStatus gs_dense_forward(GsContext *ctx, const GsDenseLayer *layer, int64_t rows, const void *x, int64_t ld_x,
+                          const void *residual, int64_t ld_residual, void *y, int64_t ld_y, void *preact, int64_t ld_preact,
+                          void *stream);
+/* The gradients of gs_dense_forward from dL_dy [rows, out_features]: with dz = dL_dy act'(preact),
+ *   dL_dx = dz W [rows, in_features];  dL_dweight = dz^T x [out_features, in_features] fp32, contiguous;
+ *   dL_dbias = sum over rows of dz [out_features] fp32.
+ * (dL/dresidual is dL_dy.)  dL_dx, or dL_dweight and dL_dbias, or dL_dbias alone, may be NULL; x may be then without
+ * dL_dweight.  preact [rows, out_features] is needed unless the activation is GS_DENSE_NONE.  dz is carried to fp32's accuracy
+ * (bf16: 24 bits in dL_dweight and 16 in dL_dx, fp16: 22); in fp16 a dz beyond 65504 makes what it enters not finite.  The
+ * derivative of ReLU at 0 is 0.  Same bits from run to run.  workspace: gs_dense_workspace_bytes(), 16-byte aligned, contents
+ * irrelevant; may be NULL without dL_dweight.  GS_ERR_CAPACITY, nothing launched, if it is smaller. */
+size_t gs_dense_workspace_bytes(int64_t rows, int32_t in_features, int32_t out_features);
+GsStatus gs_dense_backward(GsContext *ctx, const GsDenseLayer *layer, int64_t rows, const void *x, int64_t ld_x,
+                           const void *preact, int64_t ld_preact, const void *dL_dy, int64_t ld_dy, void *dL_dx,
+                           int64_t ld_dx, float *dL_dweight, float *dL_dbias, void *workspace, size_t workspace_bytes,
+                           void *stream);
+
+/* y = (x - mean) rstd gamma + beta over each row of cols values (1 .. GS_LAYER_NORM_MAX_COLS), rstd = 1 / sqrt(var + eps),
+ * var about the mean, divided by cols.  x and y are of dtype (any GsType), gamma and beta [cols] fp32 or
+ * NULL (1 and 0); mean and rstd [rows] fp32 are what the backward wants and may be NULL.  eps > 0.  y may be x.
+ * Pointers aligned to their elements; 16-byte aligned rows are read in vectors. */
+GsStatus gs_layer_norm_forward(GsContext *ctx, int32_t dtype, int64_t rows, int32_t cols, const void *x, int64_t ld_x,
+                               const float *gamma, const float *beta, float eps, void *y, int64_t ld_y, float *mean,
+                               float *rstd, void *stream);
+/* With h = (x - mean) rstd and g = dL_dy gamma: dL_dx = rstd (g - avg(g) - h avg(g h)), averages over the row;
+ * dL_dgamma = sum over rows of dL_dy h and dL_dbeta = sum over rows of dL_dy, [cols] fp32.  Each of the three may be NULL; dL_dx may
+ * be dL_dy or x.  Same bits from run to run.  workspace: gs_layer_norm_workspace_bytes(), 16-byte aligned, contents
+ * irrelevant; may be NULL without dL_dgamma and dL_dbeta.  GS_ERR_CAPACITY, nothing launched, if it is smaller. */
+size_t gs_layer_norm_workspace_bytes(int64_t rows, int32_t cols);
+GsStatus gs_layer_norm_backward(GsContext *ctx, int32_t dtype, int64_t rows, int32_t cols, const void *dL_dy,
+                                int64_t ld_dy, const void *x, int64_t ld_x, const float *gamma, const float *mean,
+                                const float *rstd, void *dL_dx, int64_t ld_dx, float *dL_dgamma, float *dL_dbeta,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
+/* A gradient for the norm over all of them: the sum of its buffers, as in GsAdamTensor. */
+typedef struct {
+  const void *grad;               /* [count], aligned to its elements                                      */
+  void *out;                      /* gs_clip_grads only: [count], same type; may be grad                   */
+  int64_t count;
+  int32_t dtype;                  /* GsType                                                                */
+  const void *const *more_grads;  /* HOST array of num_more_grads DEVICE pointers, or NULL                 */
+  int32_t num_more_grads;         /* 0 .. GS_ADAM_MAX_MORE_GRADS                                           */
+} GsGradTensor;
+/* clip (DEVICE, two floats, 8-byte aligned) receives the norm over all elements of all tensors, sqrt(sum of s^2) with s the summed gradient,
+ * and the scale that brings it to max_norm: 1 if norm <= max_norm, else max_norm / norm; 0 if the norm is not finite or beyond
+ * fp32's range.  max_norm > 0 (infinity: the norm alone is wanted).  Squares are summed in 64 bits, the same bits from run to
+ * run.  At most GS_GRAD_MAX_TENSORS tensors (empty ones among them) and GS_GRAD_MAX_BUFFERS further buffers in a call.  workspace:
+ * gs_grad_workspace_bytes(), 16-byte aligned, contents irrelevant; GS_ERR_CAPACITY, nothing launched, if it is smaller. */
+size_t gs_grad_workspace_bytes(void);
+GsStatus gs_grad_norm(GsContext *ctx, const GsGradTensor *tensors, int32_t num_tensors, float max_norm, float *clip,
+                      void *workspace, size_t workspace_bytes, void *stream);
+/* gs_grad_norm, and out = scale s for every tensor (all zeros where the norm is not finite). */
+GsStatus gs_clip_grads(GsContext *ctx, const GsGradTensor *tensors, int32_t num_tensors, float max_norm, float *clip,
+                       void *workspace, size_t workspace_bytes, void *stream);
+/* gs_adam_step with every gradient scaled by clip[1], clip being what gs_grad_norm left on the device: clipped training without
+ * a pass over the gradients of its own.  Where clip[0] is not finite nothing is written: the step is skipped. */
+GsStatus gs_adam_step_clipped(GsContext *ctx, const GsAdamTensor *tensors, int32_t num_tensors, int64_t step,
+                              const float *clip, void *stream);
+
 /* ---- NEXT: the viewer's colour prepass of the neural model as CUDA kernels (App. C.3, "Neural") --
  * Export: gs_neural_fold folds the 17 view-independent columns of the decoder's first layer (the 16
  * encoded feature inputs and the constant degree-0 input) into 16 half-precision pre-activations per
@@ -372,6 +463,9 @@ typedef enum {
   GS_STAGE_APPEARANCE_BWD,
   GS_STAGE_ADAM,               /* fused parameter update                                        */
   GS_STAGE_PREPASS,            /* viewer-side fold / colour prepass                             */
+  GS_STAGE_DENSE,              /* dense layers, forward and backward                            */
+  GS_STAGE_LAYER_NORM,         /* layer norm, forward and backward                              */
+  GS_STAGE_GRAD_NORM,          /* norm over all gradients, clipping                             */
   GS_NUM_STAGES
 } GsStage;
 GsStatus gs_profile_enable(GsContext *ctx, int enable);

@@ -92,7 +92,8 @@ _lib.gs_appearance_backward.restype = C.c_int
 
 
 STAGES = ["preprocess_fwd", "depth_sort", "tile_offsets", "keygen", "tile_sort", "tile_ranges", "blend_fwd",
-          "blend_bwd", "preprocess_bwd", "appearance_fwd", "appearance_bwd", "adam", "prepass"]
+          "blend_bwd", "preprocess_bwd", "appearance_fwd", "appearance_bwd", "adam", "prepass", "dense", "layer_norm",
+          "grad_norm"]
 _lib.gs_profile_enable.argtypes = [_vp, C.c_int]
 _lib.gs_profile_enable.restype = C.c_int
 _lib.gs_profile_collect.argtypes = [_vp, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
@@ -527,6 +528,260 @@ def gs_adam_step(ctx: Context, tensors, step: int, stream=None) -> None:
     arr = (GsAdamTensor * max(1, len(tensors)))(*[t.c_struct() for t in tensors])
     ctx._check(_lib.gs_adam_step(ctx._h, arr, len(tensors), step, _stream_handle(stream)))
 
+
+
+# ------------------------------------------------------------------------------------------------
+# Beside the scene: dense layers, layer norm, and the clipping of all gradients (include/gs.h has the formulas).
+# ------------------------------------------------------------------------------------------------
+GS_TYPE_F32, GS_TYPE_F16, GS_TYPE_BF16 = 0, 1, 2
+GS_DENSE_NONE, GS_DENSE_RELU, GS_DENSE_SILU, GS_DENSE_GELU = 0, 1, 2, 3
+_TYPES = {torch.float32: GS_TYPE_F32, torch.float16: GS_TYPE_F16, torch.bfloat16: GS_TYPE_BF16}
+_ACTIVATIONS = {"none": GS_DENSE_NONE, "relu": GS_DENSE_RELU, "silu": GS_DENSE_SILU, "gelu": GS_DENSE_GELU}
+
+
+class GsDenseLayer(C.Structure):
+    _fields_ = [("weight", _vp), ("ld_weight", C.c_int64), ("bias", _vp), ("in_features", C.c_int32),
+                ("out_features", C.c_int32), ("dtype", C.c_int32), ("activation", C.c_int32)]
+
+
+class GsGradTensor(C.Structure):
+    _fields_ = [("grad", _vp), ("out", _vp), ("count", C.c_int64), ("dtype", C.c_int32), ("more_grads", C.POINTER(_vp)),
+                ("num_more_grads", C.c_int32)]
+
+
+_i64, _i32, _size = C.c_int64, C.c_int32, C.c_size_t
+for _name, _args, _res in (
+        ("gs_dense_forward", [_vp, C.POINTER(GsDenseLayer), _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp], C.c_int),
+        ("gs_dense_workspace_bytes", [_i64, _i32, _i32], _size),
+        ("gs_dense_backward", [_vp, C.POINTER(GsDenseLayer), _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp,
+                               _size, _vp], C.c_int),
+        ("gs_layer_norm_forward", [_vp, _i32, _i64, _i32, _vp, _i64, _vp, _vp, C.c_float, _vp, _i64, _vp, _vp, _vp], C.c_int),
+        ("gs_layer_norm_workspace_bytes", [_i64, _i32], _size),
+        ("gs_layer_norm_backward", [_vp, _i32, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp,
+                                    _size, _vp], C.c_int),
+        ("gs_grad_workspace_bytes", [], _size),
+        ("gs_grad_norm", [_vp, C.POINTER(GsGradTensor), _i32, C.c_float, _vp, _vp, _size, _vp], C.c_int),
+        ("gs_clip_grads", [_vp, C.POINTER(GsGradTensor), _i32, C.c_float, _vp, _vp, _size, _vp], C.c_int),
+        ("gs_adam_step_clipped", [_vp, C.POINTER(GsAdamTensor), _i32, _i64, _vp, _vp], C.c_int)):
+    getattr(_lib, _name).argtypes, getattr(_lib, _name).restype = _args, _res
+
+
+def _invalid(message: str):
+    raise GsError(GS_ERR_INVALID_ARG, message)
+
+
+def _stream_of(ctx: Context, stream) -> int:
+    """The given stream, or the current one of the context's device."""
+    return torch._C._cuda_getCurrentRawStream(ctx.device.index) if stream is None else stream.cuda_stream
+
+
+def _matrix(ctx: Context, t: Optional[torch.Tensor], name: str, rows: int, cols: int, dtype: torch.dtype):
+    """(address, elements from row to row) of a [rows, cols] tensor whose rows are contiguous."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.device != ctx.device:
+        _invalid(f"{name} must be a {dtype} tensor [{rows}, {cols}] on {ctx.device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
+        _invalid(f"{name}: the values of a row must be contiguous")
+    return t.data_ptr(), ld if rows > 1 else (cols + 7) // 8 * 8
+
+
+def _vector(ctx: Context, t: Optional[torch.Tensor], name: str, count: int):
+    """Address of a contiguous fp32 tensor of count values."""
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.numel() != count or t.device != ctx.device or not t.is_contiguous():
+        _invalid(f"{name} must be a contiguous float32 tensor of {count} values on {ctx.device}, "
+                 f"got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _workspace(ctx: Context, t: Optional[torch.Tensor]):
+    if t is None:
+        return None, 0
+    if t.device != ctx.device or not t.is_contiguous():
+        _invalid(f"workspace must be a contiguous tensor on {ctx.device}")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+class DenseLayer:
+    """Weights of a dense layer: weight [out, in] float16 or bfloat16 (rows a multiple of eight elements apart), bias [out]
+    float32 or None, activation "none", "relu", "silu" or "gelu" (or its GS_DENSE_ number).  Marshalling only: it holds the tensors, whose
+    values may change between calls."""
+
+    def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, activation="none"):
+        if weight.dim() != 2 or weight.dtype not in _TYPES or (weight.stride(1) != 1 and weight.shape[1] > 1) or not weight.is_cuda:
+            _invalid("weight must be a CUDA matrix [out, in] with contiguous rows")
+        if isinstance(activation, str):
+            if activation not in _ACTIVATIONS:
+                _invalid(f"unknown dense activation {activation!r}")
+            activation = _ACTIVATIONS[activation]
+        if bias is not None and (bias.dtype is not torch.float32 or bias.numel() != weight.shape[0] or not bias.is_contiguous() or
+                                 bias.device != weight.device):
+            _invalid(f"bias must be a contiguous float32 tensor of {weight.shape[0]} values beside the weight")
+        self.weight, self.bias = weight, bias
+        s = GsDenseLayer()
+        s.out_features, s.in_features = weight.shape
+        s.weight, s.ld_weight = weight.data_ptr(), weight.stride(0) if weight.shape[0] > 1 else (weight.shape[1] + 7) // 8 * 8
+        s.bias = None if bias is None else bias.data_ptr()
+        s.dtype, s.activation = _TYPES[weight.dtype], int(activation)
+        self._struct = s
+
+    @property
+    def out_features(self) -> int:
+        return self._struct.out_features
+
+    @property
+    def in_features(self) -> int:
+        return self._struct.in_features
+
+
+def gs_dense_workspace_bytes(rows: int, in_features: int, out_features: int) -> int:
+    return int(_lib.gs_dense_workspace_bytes(rows, in_features, out_features))
+
+
+def _on(ctx: Context, layer: DenseLayer):
+    if layer.weight.device != ctx.device:
+        _invalid(f"the layer's weight is on {layer.weight.device}, the context on {ctx.device}")
+
+
+def gs_dense_forward(ctx: Context, layer: DenseLayer, x: torch.Tensor, y: torch.Tensor, preact: Optional[torch.Tensor] = None,
+                     residual: Optional[torch.Tensor] = None, stream=None) -> None:
+    """y = act(x W^T + bias) + residual; preact receives x W^T + bias.  Matrices in the weight's type, rows a multiple of eight
+    elements apart; residual may be y."""
+    _on(ctx, layer)
+    s, dt, rows = layer._struct, layer.weight.dtype, x.shape[0]
+    n = s.out_features
+    px, lx = _matrix(ctx, x, "x", rows, s.in_features, dt)
+    pr, lr = _matrix(ctx, residual, "residual", rows, n, dt)
+    py, ly = _matrix(ctx, y, "y", rows, n, dt)
+    pz, lz = _matrix(ctx, preact, "preact", rows, n, dt)
+    ctx._check(_lib.gs_dense_forward(ctx._h, s, rows, px, lx, pr, lr, py, ly, pz, lz, _stream_of(ctx, stream)))
+
+
+def gs_dense_backward(ctx: Context, layer: DenseLayer, x: Optional[torch.Tensor], dL_dy: torch.Tensor,
+                      preact: Optional[torch.Tensor] = None, dL_dx: Optional[torch.Tensor] = None,
+                      dL_dweight: Optional[torch.Tensor] = None, dL_dbias: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients of gs_dense_forward; what is None is left out.  dL_dx in the weight's type, dL_dweight [out, in] and dL_dbias
+    [out] float32.  preact is needed by a layer with an activation, workspace (gs_dense_workspace_bytes) and x by dL_dweight."""
+    _on(ctx, layer)
+    s, dt, rows = layer._struct, layer.weight.dtype, dL_dy.shape[0]
+    n, k = s.out_features, s.in_features
+    px, lx = _matrix(ctx, x, "x", rows, k, dt)
+    pz, lz = _matrix(ctx, preact, "preact", rows, n, dt)
+    pd, ld = _matrix(ctx, dL_dy, "dL_dy", rows, n, dt)
+    pg, lg = _matrix(ctx, dL_dx, "dL_dx", rows, k, dt)
+    pw, nw = _workspace(ctx, workspace)
+    ctx._check(_lib.gs_dense_backward(ctx._h, s, rows, px, lx, pz, lz, pd, ld, pg, lg, _vector(ctx, dL_dweight, "dL_dweight", n * k),
+                                      _vector(ctx, dL_dbias, "dL_dbias", n), pw, nw, _stream_of(ctx, stream)))
+
+
+def gs_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
+    return int(_lib.gs_layer_norm_workspace_bytes(rows, cols))
+
+
+def _normed(t: torch.Tensor):
+    if t.dim() != 2 or t.dtype not in _TYPES:
+        _invalid("layer norm takes a float32, float16 or bfloat16 matrix")
+    return _TYPES[t.dtype], t.shape[0], t.shape[1]
+
+
+def gs_layer_norm_forward(ctx: Context, x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], y: torch.Tensor,
+                          mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                          stream=None) -> None:
+    """y = (x - mean) rstd gamma + beta over each row; mean and rstd [rows] float32 are kept for the backward.  y may be x."""
+    dtype, rows, cols = _normed(x)
+    px, lx = _matrix(ctx, x, "x", rows, cols, x.dtype)
+    py, ly = _matrix(ctx, y, "y", rows, cols, x.dtype)
+    ctx._check(_lib.gs_layer_norm_forward(ctx._h, dtype, rows, cols, px, lx, _vector(ctx, gamma, "gamma", cols),
+                                          _vector(ctx, beta, "beta", cols), eps, py, ly, _vector(ctx, mean, "mean", rows),
+                                          _vector(ctx, rstd, "rstd", rows), _stream_of(ctx, stream)))
+
+
+def gs_layer_norm_backward(ctx: Context, dL_dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor,
+                           rstd: torch.Tensor, dL_dx: Optional[torch.Tensor] = None, dL_dgamma: Optional[torch.Tensor] = None,
+                           dL_dbeta: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients of gs_layer_norm_forward; what is None is left out.  workspace (gs_layer_norm_workspace_bytes) is needed by
+    dL_dgamma and dL_dbeta.  dL_dx may be dL_dy or x."""
+    dtype, rows, cols = _normed(x)
+    pd, ld = _matrix(ctx, dL_dy, "dL_dy", rows, cols, x.dtype)
+    px, lx = _matrix(ctx, x, "x", rows, cols, x.dtype)
+    pg, lg = _matrix(ctx, dL_dx, "dL_dx", rows, cols, x.dtype)
+    pw, nw = _workspace(ctx, workspace)
+    ctx._check(_lib.gs_layer_norm_backward(ctx._h, dtype, rows, cols, pd, ld, px, lx, _vector(ctx, gamma, "gamma", cols),
+                                           _vector(ctx, mean, "mean", rows), _vector(ctx, rstd, "rstd", rows), pg, lg,
+                                           _vector(ctx, dL_dgamma, "dL_dgamma", cols), _vector(ctx, dL_dbeta, "dL_dbeta", cols),
+                                           pw, nw, _stream_of(ctx, stream)))
+
+
+GS_GRAD_MAX_TENSORS, GS_GRAD_MAX_BUFFERS = 512, 1024
+
+
+class GradTensor:
+    """One gradient of the norm over all of them: a contiguous float32, float16 or bfloat16 tensor, further buffers that are
+    added to it (the views of an iteration, as in AdamTensor), and where gs_clip_grads puts the scaled sum (may be grad)."""
+
+    def __init__(self, grad: torch.Tensor, more_grads=(), out: Optional[torch.Tensor] = None):
+        self.grad, self.more_grads, self.out = grad, list(more_grads), out
+
+
+class GradList:
+    """The gradients of a model, marshalled once for the calls of every iteration."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)              # kept alive
+        self.device = self.tensors[0].grad.device if self.tensors else None
+        self._more = []
+        arr = (GsGradTensor * max(1, len(self.tensors)))()
+        for s, t in zip(arr, self.tensors):
+            if t.grad.dtype not in _TYPES:
+                _invalid(f"gradients are float32, float16 or bfloat16, got {t.grad.dtype}")
+            for x in [t.grad, *t.more_grads] + ([t.out] if t.out is not None else []):
+                if x.dtype is not t.grad.dtype or x.numel() != t.grad.numel() or x.device != self.device or not x.is_contiguous() or not x.is_cuda:
+                    _invalid("the buffers of a gradient must be contiguous CUDA tensors of one type, size and device")
+            more = (_vp * max(1, len(t.more_grads)))(*[g.data_ptr() for g in t.more_grads])
+            self._more.append(more)
+            s.grad, s.out, s.count, s.dtype = t.grad.data_ptr(), t.out.data_ptr() if t.out is not None else None, t.grad.numel(), _TYPES[t.grad.dtype]
+            s.more_grads = C.cast(more, C.POINTER(_vp)) if t.more_grads else None
+            s.num_more_grads = len(t.more_grads)
+        self._arr = arr
+
+    def __len__(self) -> int:
+        return len(self.tensors)
+
+
+def gs_grad_workspace_bytes() -> int:
+    return int(_lib.gs_grad_workspace_bytes())
+
+
+def _grads(ctx: Context, tensors) -> GradList:
+    if not isinstance(tensors, GradList):
+        tensors = GradList(tensors)
+    if tensors.device is not None and tensors.device != ctx.device:
+        _invalid(f"the gradients are on {tensors.device}, the context on {ctx.device}")
+    return tensors
+
+
+def gs_grad_norm(ctx: Context, tensors, max_norm: float, clip: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """clip[0] receives the norm over all gradients (a GradList, or GradTensors), clip[1] the scale that brings it to max_norm."""
+    g = _grads(ctx, tensors)
+    pw, nw = _workspace(ctx, workspace)
+    ctx._check(_lib.gs_grad_norm(ctx._h, g._arr, len(g), max_norm, _vector(ctx, clip, "clip", 2), pw, nw, _stream_of(ctx, stream)))
+
+
+def gs_clip_grads(ctx: Context, tensors, max_norm: float, clip: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """gs_grad_norm, and every GradTensor's out receives its summed gradient times clip[1]."""
+    g = _grads(ctx, tensors)
+    pw, nw = _workspace(ctx, workspace)
+    ctx._check(_lib.gs_clip_grads(ctx._h, g._arr, len(g), max_norm, _vector(ctx, clip, "clip", 2), pw, nw, _stream_of(ctx, stream)))
+
+
+def gs_adam_step_clipped(ctx: Context, tensors, step: int, clip: torch.Tensor, stream=None) -> None:
+    """gs_adam_step with every gradient scaled by clip[1] (from gs_grad_norm); skipped where clip[0] is not finite."""
+    arr = (GsAdamTensor * max(1, len(tensors)))(*[t.c_struct() for t in tensors])
+    ctx._check(_lib.gs_adam_step_clipped(ctx._h, arr, len(tensors), step, _vector(ctx, clip, "clip", 2), _stream_of(ctx, stream)))
 
 # ------------------------------------------------------------------------------------------------
 # The allocation-free neural appearance backward (no context, static device scratch in the library).

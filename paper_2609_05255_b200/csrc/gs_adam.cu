@@ -46,12 +46,18 @@ __device__ __forceinline__ void adam_element(float &p, float g, float &m, float 
 // kMore: some tensor has further gradients.  They are fetched two buffers and four vectors at a time and added in their order; one
 // after another, each waited for the one before: 1M Gaussians, eight gradient buffers, 1.25 GB 370 -> 208 us.  (In a kernel of its
 // own: the plain one has every load of a chunk in flight at once and 97 % of the copy rate.)
-template <bool kMore>
-__global__ void __launch_bounds__(kAdamThreads) k_adam(const __grid_constant__ AdamArgs a) {
+// kClip: the summed gradient is scaled by clip[1] (what k_grad_norm left); nothing is written if the norm clip[0] is not finite.
+template <bool kMore, bool kClip>
+__global__ void __launch_bounds__(kAdamThreads) k_adam(const __grid_constant__ AdamArgs a, const float *clip) {
   // the per-column step sizes of the chunk's tensor, in shared memory: the lanes of a warp want
   // different columns, which the constant bank would serve one address at a time
   __shared__ float s_step[GS_ADAM_MAX_COLS];
   dependency_wait();
+  float scale = 1.f;
+  if (kClip) {
+    if (!isfinite(__ldg(clip))) return;
+    scale = __ldg(clip + 1);
+  }
   const uint32_t total_chunks = a.chunk_start[a.num_tensors];
   for (uint32_t chunk = blockIdx.x; chunk < total_chunks; chunk += gridDim.x) {
     int ti = 0;
@@ -103,9 +109,10 @@ __global__ void __launch_bounds__(kAdamThreads) k_adam(const __grid_constant__ A
       if (full[u]) {
         uint32_t c = e[u] % t.cols;
         float *pp = &p[u].x, *mm = &m[u].x, *vv = &v[u].x;
-        const float *gg = &g[u].x;
+        float *gg = &g[u].x;
 #pragma unroll
         for (int k = 0; k < kAdamVec; ++k) {
+          if (kClip) gg[k] *= scale;
           adam_element(pp[k], gg[k], mm[k], vv[k], s_step[c], t.beta1, t.beta2, t.eps, t.inv_sqrt_c2);
           c = (c + 1 == t.cols) ? 0u : c + 1;
         }
@@ -124,6 +131,7 @@ __global__ void __launch_bounds__(kAdamThreads) k_adam(const __grid_constant__ A
         for (uint32_t i = e[u]; i < t.count; ++i) {
           float pv = t.param[i], mv = t.m[i], vv = t.v[i], gv = t.grad[i];
           for (int k = 0; k < t.num_more; ++k) gv += t.more[k][i];
+          if (kClip) gv *= scale;
           adam_element(pv, gv, mv, vv, s_step[c], t.beta1, t.beta2, t.eps, t.inv_sqrt_c2);
           t.param[i] = pv; t.m[i] = mv; t.v[i] = vv;
           if (t.half_copy) t.half_copy[i] = __float2half_rn(pv);
@@ -136,9 +144,9 @@ __global__ void __launch_bounds__(kAdamThreads) k_adam(const __grid_constant__ A
 
 }  // namespace
 
-// Host side of gs_adam_step: validates nothing (the C entry point does), fills the argument block,
-// launches.  Returns the number of kernels launched.
-int launch_adam(const GsAdamTensor *tensors, int num_tensors, int64_t step, int num_sms, cudaStream_t st) {
+// Host side of gs_adam_step and, with clip, of gs_adam_step_clipped: validates nothing (the C entry point does), fills the
+// argument block, launches.  Returns the number of kernels launched.
+int launch_adam(const GsAdamTensor *tensors, int num_tensors, int64_t step, const float *clip, int num_sms, cudaStream_t st) {
   AdamArgs a;
   bool more = false;
   a.num_tensors = 0;
@@ -164,7 +172,9 @@ int launch_adam(const GsAdamTensor *tensors, int num_tensors, int64_t step, int 
   const uint32_t chunks = a.chunk_start[a.num_tensors];
   if (chunks == 0) return 0;
   const uint32_t wave = (uint32_t)num_sms * 8u;
-  launch_chained(more ? k_adam<true> : k_adam<false>, chunks < wave ? chunks : wave, kAdamThreads, 0, st, a);
+  const uint32_t grid = chunks < wave ? chunks : wave;
+  if (clip) launch_chained(more ? k_adam<true, true> : k_adam<false, true>, grid, kAdamThreads, 0, st, a, clip);
+  else launch_chained(more ? k_adam<true, false> : k_adam<false, false>, grid, kAdamThreads, 0, st, a, clip);
   return 1;
 }
 

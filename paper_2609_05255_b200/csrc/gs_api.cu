@@ -55,7 +55,7 @@ GsStatus check_cuda(GsContext *ctx, cudaError_t e, const char *what) {
 
 const char *const kStageNames[] = {"preprocess_fwd", "depth_sort", "tile_offsets", "keygen", "tile_sort", "tile_ranges",
                                    "blend_fwd", "blend_bwd", "preprocess_bwd", "appearance_fwd", "appearance_bwd",
-                                   "adam", "prepass"};
+                                   "adam", "prepass", "dense", "layer_norm", "grad_norm"};
 static_assert(sizeof(kStageNames) / sizeof(kStageNames[0]) == GS_NUM_STAGES, "one name per stage");
 
 // Brackets one stage with events, and with an NVTX range for a tracing tool, when profiling is on.
@@ -714,7 +714,8 @@ GsStatus gs_profile_blend_counts(GsContext *ctx, const GsProjected *proj, const 
   return GS_OK;
 }
 
-GsStatus gs_adam_step(GsContext *ctx, const GsAdamTensor *tensors, int32_t num_tensors, int64_t step, void *stream) {
+namespace {
+GsStatus adam_impl(GsContext *ctx, const GsAdamTensor *tensors, int32_t num_tensors, int64_t step, const float *clip, void *stream) {
   if (!ctx) return GS_ERR_INVALID_ARG;
   if (num_tensors < 0 || num_tensors > GS_ADAM_MAX_TENSORS || (num_tensors > 0 && !tensors))
     return fail(ctx, GS_ERR_INVALID_ARG, "num_tensors must be 0..8 and tensors non-NULL");
@@ -739,9 +740,242 @@ GsStatus gs_adam_step(GsContext *ctx, const GsAdamTensor *tensors, int32_t num_t
   cudaSetDevice(ctx->device);
   {
     StageTimer t(ctx, GS_STAGE_ADAM, s);
-    t.done(launch_adam(tensors, num_tensors, step, ctx->num_sms, s));
+    t.done(launch_adam(tensors, num_tensors, step, clip, ctx->num_sms, s));
   }
   return check_cuda(ctx, cudaGetLastError(), "adam launch");
+}
+}  // namespace
+GsStatus gs_adam_step(GsContext *ctx, const GsAdamTensor *tensors, int32_t num_tensors, int64_t step, void *stream) {
+  return adam_impl(ctx, tensors, num_tensors, step, nullptr, stream);
+}
+GsStatus gs_adam_step_clipped(GsContext *ctx, const GsAdamTensor *tensors, int32_t num_tensors, int64_t step, const float *clip, void *stream) {
+  if (!ctx) return GS_ERR_INVALID_ARG;
+  if (!clip || (reinterpret_cast<uintptr_t>(clip) & 7u)) return fail(ctx, GS_ERR_INVALID_ARG, "clip is NULL or misaligned");
+  return adam_impl(ctx, tensors, num_tensors, step, clip, stream);
+}
+
+// ---- layers and clipping ----------------------------------------------------------------------------
+namespace {
+size_t type_bytes(int dtype) { return dtype == GS_TYPE_F32 ? 4 : 2; }
+bool type_ok(int dtype) { return dtype == GS_TYPE_F32 || dtype == GS_TYPE_F16 || dtype == GS_TYPE_BF16; }
+bool element_aligned(const void *p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (type_bytes(dtype) - 1)) == 0; }
+
+// The context's device for the length of a call; the caller's current one afterwards.
+struct OnDevice {
+  int before = -1;
+  explicit OnDevice(int device) {
+    if (cudaGetDevice(&before) != cudaSuccess) before = -1;
+    if (before != device) cudaSetDevice(device); else before = -1;
+  }
+  ~OnDevice() { if (before >= 0) cudaSetDevice(before); }
+};
+
+GsStatus dense_ok(GsContext *ctx, const GsDenseLayer *l, int64_t rows) {
+  if (!l) return fail(ctx, GS_ERR_INVALID_ARG, "layer is NULL");
+  if (l->dtype != GS_TYPE_F16 && l->dtype != GS_TYPE_BF16)
+    return fail(ctx, type_ok(l->dtype) ? GS_ERR_UNSUPPORTED : GS_ERR_INVALID_ARG, "dense layers are fp16 or bf16");
+  if (l->activation < GS_DENSE_NONE || l->activation > GS_DENSE_GELU) return fail(ctx, GS_ERR_INVALID_ARG, "unknown dense activation");
+  if (l->in_features < 1 || l->in_features > GS_DENSE_MAX_FEATURES || l->out_features < 1 || l->out_features > GS_DENSE_MAX_FEATURES)
+    return fail(ctx, GS_ERR_INVALID_ARG, "in_features and out_features must be 1..16384");
+  if (rows < 0) return fail(ctx, GS_ERR_INVALID_ARG, "rows < 0");
+  if (rows >= ((int64_t)1 << 31)) return fail(ctx, GS_ERR_CAPACITY, "rows must stay below 2^31");
+  if (bad_ptr(l->weight) || l->ld_weight < l->in_features || (l->ld_weight & 7))
+    return fail(ctx, GS_ERR_INVALID_ARG, "weight is NULL or misaligned, or ld_weight is no multiple of 8 or shorter than a row");
+  if (l->bias && (reinterpret_cast<uintptr_t>(l->bias) & 3u)) return fail(ctx, GS_ERR_INVALID_ARG, "bias is misaligned");
+  return GS_OK;
+}
+// A matrix that moves by TMA.
+bool matrix_bad(const void *p, int64_t ld, int32_t cols) { return bad_ptr(p) || ld < cols || (ld & 7) || ld >= ((int64_t)1 << 38); }
+
+GsStatus grads_ok(GsContext *ctx, const GsGradTensor *tensors, int32_t num_tensors, bool scale, float max_norm, const float *clip, const void *workspace,
+                  size_t workspace_bytes) {
+  if (num_tensors < 0 || num_tensors > GS_GRAD_MAX_TENSORS || (num_tensors > 0 && !tensors))
+    return fail(ctx, GS_ERR_INVALID_ARG, "num_tensors must be 0..512 and tensors non-NULL");
+  if (!(max_norm > 0.f)) return fail(ctx, GS_ERR_INVALID_ARG, "max_norm must be above 0");
+  if (!clip || (reinterpret_cast<uintptr_t>(clip) & 7u)) return fail(ctx, GS_ERR_INVALID_ARG, "clip is NULL or misaligned");
+  int64_t more = 0, chunks = 0;
+  for (int i = 0; i < num_tensors; ++i) {
+    const GsGradTensor &t = tensors[i];
+    if (t.count < 0 || !type_ok(t.dtype)) return fail(ctx, GS_ERR_INVALID_ARG, "a gradient's count is below 0 or its type unknown");
+    if (t.num_more_grads < 0 || t.num_more_grads > GS_ADAM_MAX_MORE_GRADS || (t.num_more_grads > 0 && !t.more_grads))
+      return fail(ctx, GS_ERR_INVALID_ARG, "num_more_grads outside 0..7 or more_grads is NULL");
+    if (t.count == 0) continue;
+    if (t.count >= ((int64_t)1 << 40)) return fail(ctx, GS_ERR_CAPACITY, "a gradient has 2^40 elements or more");
+    if (!t.grad || !element_aligned(t.grad, t.dtype) || (scale && (!t.out || !element_aligned(t.out, t.dtype))))
+      return fail(ctx, GS_ERR_INVALID_ARG, "a gradient or its out is NULL or misaligned");
+    for (int k = 0; k < t.num_more_grads; ++k)
+      if (!t.more_grads[k] || !element_aligned(t.more_grads[k], t.dtype)) return fail(ctx, GS_ERR_INVALID_ARG, "a further gradient pointer is NULL or misaligned");
+    more += t.num_more_grads;
+    chunks += (t.count >> 13) + 1;
+  }
+  if (more > GS_GRAD_MAX_BUFFERS) return fail(ctx, GS_ERR_INVALID_ARG, "more than 1024 further gradient buffers");
+  if (chunks >= ((int64_t)1 << 31)) return fail(ctx, GS_ERR_CAPACITY, "the gradients have 2^44 elements or more");
+  if (bad_ptr(workspace)) return fail(ctx, GS_ERR_INVALID_ARG, "workspace is NULL or misaligned");
+  if (workspace_bytes < gs_grad_workspace_bytes()) return fail(ctx, GS_ERR_CAPACITY, "workspace smaller than gs_grad_workspace_bytes()");
+  return GS_OK;
+}
+GsStatus grads_impl(GsContext *ctx, const GsGradTensor *tensors, int32_t num_tensors, bool scale, float max_norm, float *clip, void *workspace,
+                    size_t workspace_bytes, void *stream) {
+  if (!ctx) return GS_ERR_INVALID_ARG;
+  const GsStatus st = grads_ok(ctx, tensors, num_tensors, scale, max_norm, clip, workspace, workspace_bytes);
+  if (st != GS_OK) return st;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  OnDevice on(ctx->device);
+  {
+    StageTimer t(ctx, GS_STAGE_GRAD_NORM, s);
+    t.done(launch_grad_clip(tensors, num_tensors, scale, max_norm, clip, static_cast<double *>(workspace), ctx->num_sms, s));
+  }
+  return check_cuda(ctx, cudaGetLastError(), "gradient norm launch");
+}
+}  // namespace
+
+size_t gs_grad_workspace_bytes(void) { return sizeof(double) * kGradPartials; }
+GsStatus gs_grad_norm(GsContext *ctx, const GsGradTensor *tensors, int32_t num_tensors, float max_norm, float *clip, void *workspace,
+                      size_t workspace_bytes, void *stream) {
+  return grads_impl(ctx, tensors, num_tensors, false, max_norm, clip, workspace, workspace_bytes, stream);
+}
+GsStatus gs_clip_grads(GsContext *ctx, const GsGradTensor *tensors, int32_t num_tensors, float max_norm, float *clip, void *workspace,
+                       size_t workspace_bytes, void *stream) {
+  return grads_impl(ctx, tensors, num_tensors, true, max_norm, clip, workspace, workspace_bytes, stream);
+}
+
+GsStatus gs_dense_forward(GsContext *ctx, const GsDenseLayer *layer, int64_t rows, const void *x, int64_t ld_x, const void *residual,
+                          int64_t ld_residual, void *y, int64_t ld_y, void *preact, int64_t ld_preact, void *stream) {
+  if (!ctx) return GS_ERR_INVALID_ARG;
+  const GsStatus st = dense_ok(ctx, layer, rows);
+  if (st != GS_OK || rows == 0) return st;
+  if (matrix_bad(x, ld_x, layer->in_features) || matrix_bad(y, ld_y, layer->out_features) ||
+      (residual && matrix_bad(residual, ld_residual, layer->out_features)) || (preact && matrix_bad(preact, ld_preact, layer->out_features)))
+    return fail(ctx, GS_ERR_INVALID_ARG, "a matrix is NULL or misaligned, or its ld is no multiple of 8 or shorter than a row");
+  DenseArgs a = {};
+  a.rows = rows; a.in = layer->in_features; a.out = layer->out_features; a.dtype = layer->dtype; a.act = layer->activation;
+  a.x = x; a.w = layer->weight; a.residual = residual; a.ld_x = ld_x; a.ld_w = layer->ld_weight; a.ld_residual = ld_residual;
+  a.ld_preact = ld_preact; a.ld_y = ld_y; a.bias = layer->bias; a.y = y; a.preact = preact;
+  a.timeout = ctx->d_counter + 3;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  OnDevice on(ctx->device);
+  int launches;
+  {
+    StageTimer t(ctx, GS_STAGE_DENSE, s);
+    launches = launch_dense_fwd(a, ctx->num_sms, s);
+    t.done(launches);
+  }
+  if (launches < 0) return fail(ctx, GS_ERR_INTERNAL, "the driver refused a tensor map");
+  return check_cuda(ctx, cudaGetLastError(), "dense forward launch");
+}
+
+size_t gs_dense_workspace_bytes(int64_t rows, int32_t in_features, int32_t out_features) {
+  if (rows < 0 || rows >= ((int64_t)1 << 31) || in_features < 1 || in_features > GS_DENSE_MAX_FEATURES || out_features < 1 ||
+      out_features > GS_DENSE_MAX_FEATURES)
+    return 0;
+  return sizeof(float) * dense_partials(rows, in_features, out_features);
+}
+
+GsStatus gs_dense_backward(GsContext *ctx, const GsDenseLayer *layer, int64_t rows, const void *x, int64_t ld_x, const void *preact,
+                           int64_t ld_preact, const void *dL_dy, int64_t ld_dy, void *dL_dx, int64_t ld_dx, float *dL_dweight, float *dL_dbias,
+                           void *workspace, size_t workspace_bytes, void *stream) {
+  if (!ctx) return GS_ERR_INVALID_ARG;
+  const GsStatus st = dense_ok(ctx, layer, rows);
+  if (st != GS_OK) return st;
+  const int in = layer->in_features, out = layer->out_features;
+  if (dL_dbias && !dL_dweight) return fail(ctx, GS_ERR_INVALID_ARG, "dL_dbias comes with dL_dweight");
+  if ((reinterpret_cast<uintptr_t>(dL_dweight) | reinterpret_cast<uintptr_t>(dL_dbias)) & 3u) return fail(ctx, GS_ERR_INVALID_ARG, "dL_dweight or dL_dbias is misaligned");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (rows == 0) {
+    OnDevice on(ctx->device);
+    if (dL_dweight) cudaMemsetAsync(dL_dweight, 0, sizeof(float) * (size_t)in * out, s);
+    if (dL_dbias) cudaMemsetAsync(dL_dbias, 0, sizeof(float) * (size_t)out, s);
+    return check_cuda(ctx, cudaGetLastError(), "dense backward of no rows");
+  }
+  if (matrix_bad(dL_dy, ld_dy, out) || (layer->activation != GS_DENSE_NONE && matrix_bad(preact, ld_preact, out)) ||
+      (dL_dweight && matrix_bad(x, ld_x, in)) || (dL_dx && matrix_bad(dL_dx, ld_dx, in)))
+    return fail(ctx, GS_ERR_INVALID_ARG, "a matrix is NULL or misaligned, or its ld is no multiple of 8 or shorter than a row");
+  if (dL_dweight && bad_ptr(workspace)) return fail(ctx, GS_ERR_INVALID_ARG, "workspace is NULL or misaligned");
+  if (dL_dweight && workspace_bytes < gs_dense_workspace_bytes(rows, in, out))
+    return fail(ctx, GS_ERR_CAPACITY, "workspace smaller than gs_dense_workspace_bytes()");
+  DenseArgs a = {};
+  a.rows = rows; a.in = in; a.out = out; a.dtype = layer->dtype; a.act = layer->activation;
+  a.x = x; a.w = layer->weight; a.preact_in = preact; a.dy = dL_dy; a.ld_x = ld_x; a.ld_w = layer->ld_weight; a.ld_preact = ld_preact;
+  a.ld_dy = ld_dy; a.ld_dx = ld_dx; a.dx = dL_dx; a.dw = dL_dweight; a.db = dL_dbias; a.partials = static_cast<float *>(workspace);
+  a.timeout = ctx->d_counter + 3;
+  OnDevice on(ctx->device);
+  int launches;
+  {
+    StageTimer t(ctx, GS_STAGE_DENSE, s);
+    launches = launch_dense_bwd(a, ctx->num_sms, s);
+    t.done(launches);
+  }
+  if (launches < 0) return fail(ctx, GS_ERR_INTERNAL, "the driver refused a tensor map");
+  return check_cuda(ctx, cudaGetLastError(), "dense backward launch");
+}
+
+namespace {
+GsStatus norm_ok(GsContext *ctx, int32_t dtype, int64_t rows, int32_t cols) {
+  if (!type_ok(dtype)) return fail(ctx, GS_ERR_INVALID_ARG, "unknown type");
+  if (rows < 0 || cols < 1 || cols > GS_LAYER_NORM_MAX_COLS) return fail(ctx, GS_ERR_INVALID_ARG, "rows < 0 or cols outside 1..8192");
+  if (rows >= ((int64_t)1 << 31)) return fail(ctx, GS_ERR_CAPACITY, "rows must stay below 2^31");
+  return GS_OK;
+}
+bool rows_bad(const void *p, int64_t ld, int32_t cols, int dtype) { return !p || !element_aligned(p, dtype) || ld < cols; }
+bool floats_bad(const float *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+}  // namespace
+
+GsStatus gs_layer_norm_forward(GsContext *ctx, int32_t dtype, int64_t rows, int32_t cols, const void *x, int64_t ld_x, const float *gamma,
+                               const float *beta, float eps, void *y, int64_t ld_y, float *mean, float *rstd, void *stream) {
+  if (!ctx) return GS_ERR_INVALID_ARG;
+  const GsStatus st = norm_ok(ctx, dtype, rows, cols);
+  if (st != GS_OK) return st;
+  if (!(eps > 0.f)) return fail(ctx, GS_ERR_INVALID_ARG, "eps must be above 0");
+  if (rows == 0) return GS_OK;
+  if (rows_bad(x, ld_x, cols, dtype) || rows_bad(y, ld_y, cols, dtype)) return fail(ctx, GS_ERR_INVALID_ARG, "x or y is NULL or misaligned, or its ld shorter than a row");
+  if (floats_bad(gamma) || floats_bad(beta) || floats_bad(mean) || floats_bad(rstd)) return fail(ctx, GS_ERR_INVALID_ARG, "a vector is misaligned");
+  LayerNormArgs a = {};
+  a.rows = rows; a.cols = cols; a.dtype = dtype; a.x = x; a.y = y; a.ld_x = ld_x; a.ld_out = ld_y; a.gamma = gamma; a.beta = beta;
+  a.mean = mean; a.rstd = rstd; a.eps = eps;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  OnDevice on(ctx->device);
+  {
+    StageTimer t(ctx, GS_STAGE_LAYER_NORM, s);
+    t.done(launch_layer_norm_fwd(a, ctx->num_sms, s));
+  }
+  return check_cuda(ctx, cudaGetLastError(), "layer norm launch");
+}
+
+size_t gs_layer_norm_workspace_bytes(int64_t rows, int32_t cols) {
+  if (rows < 0 || cols < 1 || cols > GS_LAYER_NORM_MAX_COLS) return 0;
+  return sizeof(float) * layer_norm_partials(rows > 0 ? rows : 1, cols);
+}
+
+GsStatus gs_layer_norm_backward(GsContext *ctx, int32_t dtype, int64_t rows, int32_t cols, const void *dL_dy, int64_t ld_dy, const void *x,
+                                int64_t ld_x, const float *gamma, const float *mean, const float *rstd, void *dL_dx, int64_t ld_dx,
+                                float *dL_dgamma, float *dL_dbeta, void *workspace, size_t workspace_bytes, void *stream) {
+  if (!ctx) return GS_ERR_INVALID_ARG;
+  const GsStatus st = norm_ok(ctx, dtype, rows, cols);
+  if (st != GS_OK) return st;
+  if (floats_bad(gamma) || floats_bad(mean) || floats_bad(rstd) || floats_bad(dL_dgamma) || floats_bad(dL_dbeta))
+    return fail(ctx, GS_ERR_INVALID_ARG, "a vector is misaligned");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (rows == 0) {
+    OnDevice on(ctx->device);
+    if (dL_dgamma) cudaMemsetAsync(dL_dgamma, 0, sizeof(float) * (size_t)cols, s);
+    if (dL_dbeta) cudaMemsetAsync(dL_dbeta, 0, sizeof(float) * (size_t)cols, s);
+    return check_cuda(ctx, cudaGetLastError(), "layer norm backward of no rows");
+  }
+  if (rows_bad(dL_dy, ld_dy, cols, dtype) || rows_bad(x, ld_x, cols, dtype) || (dL_dx && rows_bad(dL_dx, ld_dx, cols, dtype)) || !mean || !rstd)
+    return fail(ctx, GS_ERR_INVALID_ARG, "dL_dy, x, dL_dx, mean or rstd is NULL or misaligned, or an ld shorter than a row");
+  if ((dL_dgamma || dL_dbeta) && bad_ptr(workspace)) return fail(ctx, GS_ERR_INVALID_ARG, "workspace is NULL or misaligned");
+  if ((dL_dgamma || dL_dbeta) && workspace_bytes < gs_layer_norm_workspace_bytes(rows, cols))
+    return fail(ctx, GS_ERR_CAPACITY, "workspace smaller than gs_layer_norm_workspace_bytes()");
+  LayerNormArgs a = {};
+  a.rows = rows; a.cols = cols; a.dtype = dtype; a.x = x; a.dy = dL_dy; a.dx = dL_dx; a.ld_x = ld_x; a.ld_dy = ld_dy; a.ld_out = ld_dx;
+  a.gamma = gamma; a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd); a.dgamma = dL_dgamma; a.dbeta = dL_dbeta;
+  a.partials = static_cast<float *>(workspace);
+  OnDevice on(ctx->device);
+  {
+    StageTimer t(ctx, GS_STAGE_LAYER_NORM, s);
+    t.done(launch_layer_norm_bwd(a, ctx->num_sms, s));
+  }
+  return check_cuda(ctx, cudaGetLastError(), "layer norm backward launch");
 }
 
 GsStatus gs_neural_fold(GsContext *ctx, const GsScene *scene, uint16_t *preact, void *stream) {

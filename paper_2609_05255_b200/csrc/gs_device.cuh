@@ -282,7 +282,44 @@ int launch_neural_fold(int64_t n, const __half *features, const __half *weights,
 int launch_neural_prepass(int64_t n, int deg, int act, const float *means, const float *logits, const float *base_color,
                           const __half *preact, const __half *weights, const float eye[3], uint8_t *rgba, float *color,
                           cudaStream_t st);
-int launch_adam(const GsAdamTensor *tensors, int num_tensors, int64_t step, int num_sms, cudaStream_t st);
+int launch_adam(const GsAdamTensor *tensors, int num_tensors, int64_t step, const float *clip, int num_sms, cudaStream_t st);
+constexpr int kGradPartials = 2048;  // most CTAs of the gradient norm: a sum of squares in 64 bits of each
+int launch_grad_clip(const GsGradTensor *tensors, int num_tensors, bool scale, float max_norm, float *clip, double *partials, int num_sms,
+                     cudaStream_t st);
+
+// Layer norm over rows (gs_layer_norm.cu).
+struct LayerNormArgs {
+  int64_t rows;
+  int cols, dtype;
+  const void *x, *dy;
+  void *y, *dx;                // y forward, dx backward
+  int64_t ld_x, ld_dy, ld_out; // elements from row to row; ld_out of y or dx
+  const float *gamma, *beta;   // may be null
+  float *mean, *rstd;          // forward: may be null
+  float eps;
+  float *dgamma, *dbeta;       // backward: may be null
+  float *partials;
+};
+size_t layer_norm_partials(int64_t rows, int cols);   // floats of workspace that the backward needs
+int launch_layer_norm_fwd(const LayerNormArgs &a, int num_sms, cudaStream_t st);
+int launch_layer_norm_bwd(const LayerNormArgs &a, int num_sms, cudaStream_t st);
+
+// Dense layers (gs_dense.cu).
+struct DenseArgs {
+  int64_t rows;
+  int in, out, dtype, act;
+  const void *x, *w, *residual, *preact_in, *dy;
+  int64_t ld_x, ld_w, ld_residual, ld_preact, ld_dy, ld_y, ld_dx;
+  const float *bias;
+  void *y, *preact, *dx;
+  float *dw, *db;
+  float *partials;
+  unsigned long long *timeout;   // set to 1 if a bounded wait ran out (never expected)
+};
+size_t dense_partials(int64_t rows, int in, int out);  // floats of workspace that the backward needs
+// The number of kernels launched, or -1 if a tensor map could not be made.
+int launch_dense_fwd(const DenseArgs &a, int num_sms, cudaStream_t st);
+int launch_dense_bwd(const DenseArgs &a, int num_sms, cudaStream_t st);
 int launch_blend_count(const CamDev &cam, const uint32_t *ranges, const uint32_t *vals, const float *mean2d,
                        const float *conic_opacity, const float *color, unsigned long long *counts, cudaStream_t st);
 

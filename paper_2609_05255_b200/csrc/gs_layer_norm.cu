@@ -1,0 +1,346 @@
+// Layer norm over the rows of a matrix, forward and backward.
+//
+//   mean, var of a row;  rstd = 1 / sqrt(var + eps);  h = (x - mean) rstd;  y = h gamma + beta
+//   backward: g = dy gamma;  dx = rstd (g - avg(g) - h avg(g h));  dgamma = sum over rows of dy h;  dbeta = sum over rows of dy
+//
+// A pure stream: forward reads x and writes y once, backward reads x and dy and writes dx once, so HBM bounds it.  A row
+// lives in the registers of a group of lanes (1 to 32 of a warp, or the 256 of a CTA), as the vectors of 16 bytes it was
+// loaded in; the variance is taken about the mean in a second pass over the registers, which loses nothing where the mean is
+// large against the spread.  All sums in fp32.  The grid is persistent: a lane keeps its columns from row to row, so
+// gamma and beta stay in registers, and in the backward so do its sums for dgamma and dbeta, which leave as one row of partial
+// sums per CTA and are added up by k_layer_norm_sums in a fixed order (no atomics: the same bits from run to run).
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "gs_device.cuh"
+
+namespace gs {
+namespace {
+
+#include "gs_rows.cuh"
+
+constexpr int kNormThreads = 256;
+constexpr int kNormPartialRows = 592;     // most CTAs of the backward
+
+// How a row is laid over lanes: `lanes` of them with NV vectors of V elements each, vector j of lane l at column (j lanes + l) V.
+template <class T, int V, int NV, bool kBlock>
+struct Row {
+  uint4 raw[V > 1 ? NV : 1];
+  float one[V > 1 ? 1 : NV];
+  // whole vectors; of the row's last one what is there (zero beyond)
+  __device__ __forceinline__ void load(const T *p, int lane, int lanes, int cols, bool live) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (j * lanes + lane) * V;
+      if constexpr (V > 1) {
+        raw[j] = make_uint4(0u, 0u, 0u, 0u);
+        if (live && c + V <= cols) raw[j] = __ldcs(reinterpret_cast<const uint4 *>(p + c));
+        else if (live && c < cols) {
+          float v[V];
+#pragma unroll
+          for (int i = 0; i < V; ++i) v[i] = c + i < cols ? widen(p[c + i]) : 0.f;
+          raw[j] = pack<T>(v);
+        }
+      } else {
+        one[j] = live && c < cols ? widen(p[c]) : 0.f;
+      }
+    }
+  }
+  __device__ __forceinline__ void get(int j, float v[V]) const {
+    if constexpr (V > 1) unpack<T>(raw[j], v);
+    else v[0] = one[j];
+  }
+};
+template <class T, int V>
+__device__ __forceinline__ void put(T *p, int c, int cols, const float v[V]) {
+  if constexpr (V > 1) {
+    if (c + V <= cols) { __stcs(reinterpret_cast<uint4 *>(p + c), pack<T>(v)); return; }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (c + i < cols) p[c + i] = narrow<T>(v[i]);
+}
+
+// Sum over a group; in the order of the lanes' numbers, the same in every lane.
+template <bool kBlock>
+__device__ __forceinline__ float group_sum(float v, int lanes, float *shared) {
+  if constexpr (!kBlock) {
+    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  } else {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = shared[0];
+#pragma unroll
+    for (int w = 1; w < kNormThreads / 32; ++w) v += shared[w];
+    return v;
+  }
+}
+template <bool kBlock>
+__device__ __forceinline__ float2 group_sum2(float2 v, int lanes, float *shared) {
+  const float a = group_sum<kBlock>(v.x, lanes, shared);
+  return make_float2(a, group_sum<kBlock>(v.y, lanes, shared));
+}
+
+// A lane's values of a parameter vector.
+template <int V, int NV>
+__device__ __forceinline__ void columns(const float *p, float fallback, int lane, int lanes, int cols, float out[V * NV]) {
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int c = (j * lanes + lane) * V + i;
+      out[j * V + i] = p && c < cols ? __ldg(p + c) : fallback;
+    }
+}
+
+template <class T, int V, int NV, bool kBlock>
+__global__ void __launch_bounds__(kNormThreads) k_layer_norm_fwd(LayerNormArgs a, int lanes) {
+  __shared__ float shared[kNormThreads / 32];
+  dependency_wait();
+  const int group = kBlock ? 0 : threadIdx.x / lanes, lane = kBlock ? threadIdx.x : threadIdx.x & (lanes - 1);
+  const int groups = kBlock ? 1 : kNormThreads / lanes;
+  float gamma[V * NV], beta[V * NV];
+  columns<V, NV>(a.gamma, 1.f, lane, lanes, a.cols, gamma);
+  columns<V, NV>(a.beta, 0.f, lane, lanes, a.cols, beta);
+  const float inv = 1.f / (float)a.cols;
+  for (int64_t row0 = (int64_t)blockIdx.x * groups; row0 < a.rows; row0 += (int64_t)gridDim.x * groups) {
+    const int64_t row = row0 + group;
+    const bool live = row < a.rows;
+    Row<T, V, NV, kBlock> x;
+    x.load(static_cast<const T *>(a.x) + row * a.ld_x, lane, lanes, a.cols, live);
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float v[V];
+      x.get(j, v);
+#pragma unroll
+      for (int i = 0; i < V; ++i) s += v[i];
+    }
+    const float mean = group_sum<kBlock>(s, lanes, shared) * inv;
+    s = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float v[V];
+      x.get(j, v);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float d = (j * lanes + lane) * V + i < a.cols ? v[i] - mean : 0.f;
+        s = fmaf(d, d, s);
+      }
+    }
+    const float rstd = 1.f / sqrtf(fmaf(group_sum<kBlock>(s, lanes, shared), inv, a.eps));
+    if (live) {
+      T *y = static_cast<T *>(a.y) + row * a.ld_out;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int c = (j * lanes + lane) * V;
+        if (c >= a.cols) break;
+        float v[V];
+        x.get(j, v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = fmaf((v[i] - mean) * rstd, gamma[j * V + i], beta[j * V + i]);
+        put<T, V>(y, c, a.cols, v);
+      }
+      if (lane == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+      }
+    }
+  }
+}
+
+template <class T, int V, int NV, bool kBlock, bool kParams>
+__global__ void __launch_bounds__(kNormThreads) k_layer_norm_bwd(LayerNormArgs a, int lanes) {
+  __shared__ float shared[kNormThreads / 32];
+  constexpr int E = V * NV;
+  dependency_wait();
+  const int group = kBlock ? 0 : threadIdx.x / lanes, lane = kBlock ? threadIdx.x : threadIdx.x & (lanes - 1);
+  const int groups = kBlock ? 1 : kNormThreads / lanes;
+  float gamma[E], sum_g[E], sum_b[E];
+  columns<V, NV>(a.gamma, 1.f, lane, lanes, a.cols, gamma);
+#pragma unroll
+  for (int i = 0; i < E; ++i) sum_g[i] = sum_b[i] = 0.f;
+  const float inv = 1.f / (float)a.cols;
+  for (int64_t row0 = (int64_t)blockIdx.x * groups; row0 < a.rows; row0 += (int64_t)gridDim.x * groups) {
+    const int64_t row = row0 + group;
+    const bool live = row < a.rows;
+    Row<T, V, NV, kBlock> x, dy;
+    x.load(static_cast<const T *>(a.x) + row * a.ld_x, lane, lanes, a.cols, live);
+    dy.load(static_cast<const T *>(a.dy) + row * a.ld_dy, lane, lanes, a.cols, live);
+    const float mean = live ? __ldg(a.mean + row) : 0.f, rstd = live ? __ldg(a.rstd + row) : 0.f;
+    float h[E], g[E];
+    float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float v[V], d[V];
+      x.get(j, v);
+      dy.get(j, d);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int e = j * V + i;
+        // columns behind the row's end have dy = 0: nothing comes of them whatever h is there
+        h[e] = (v[i] - mean) * rstd;
+        g[e] = d[i] * gamma[e];
+        s.x += g[e];
+        s.y = fmaf(g[e], h[e], s.y);
+        if (kParams) {
+          sum_g[e] = fmaf(d[i], h[e], sum_g[e]);
+          sum_b[e] += d[i];
+        }
+      }
+    }
+    s = group_sum2<kBlock>(s, lanes, shared);
+    if (live && a.dx) {
+      const float avg_g = s.x * inv, avg_gh = s.y * inv;
+      T *dx = static_cast<T *>(a.dx) + row * a.ld_out;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int c = (j * lanes + lane) * V;
+        if (c >= a.cols) break;
+        float v[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = rstd * (fmaf(-h[j * V + i], avg_gh, g[j * V + i]) - avg_g);
+        put<T, V>(dx, c, a.cols, v);
+      }
+    }
+  }
+  if constexpr (kParams) {
+    // one row [2, cols] per CTA: the groups' sums of a column added in their order
+    float *out = a.partials + (size_t)blockIdx.x * 2 * a.cols;
+    if constexpr (kBlock) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int c = ((e / V) * lanes + lane) * V + e % V;
+        if (c < a.cols) { out[c] = sum_g[e]; out[a.cols + c] = sum_b[e]; }
+      }
+    } else {
+      __shared__ float part[kNormThreads];
+      // (sums of a warp's groups by shuffles, then of the warps through shared memory)
+#pragma unroll
+      for (int e = 0; e < 2 * E; ++e) {
+        float v = e < E ? sum_g[e < E ? e : 0] : sum_b[e < E ? 0 : e - E];
+        for (int o = lanes; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        __syncthreads();
+        part[threadIdx.x] = v;
+        __syncthreads();
+        const int l = threadIdx.x, k = e % E;
+        if (l < lanes) {
+          float t = part[l];
+#pragma unroll
+          for (int w = 1; w < kNormThreads / 32; ++w) t += part[32 * w + l];
+          const int c = ((k / V) * lanes + l) * V + k % V;
+          if (c < a.cols) out[(e < E ? 0 : a.cols) + c] = t;
+        }
+      }
+    }
+  }
+}
+
+// Adds the CTAs' rows of partial sums: 32 columns per CTA, eight warps over the rows.
+__global__ void __launch_bounds__(256) k_layer_norm_sums(const float *partials, int count, int cols, float *dgamma, float *dbeta) {
+  __shared__ double part[8][32];
+  dependency_wait();
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
+  double s = 0.0;
+  if (c < 2 * cols)
+    for (int r = w; r < count; r += 8) s += (double)__ldcg(partials + (size_t)r * 2 * cols + c);
+  part[w][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (w == 0 && c < 2 * cols) {
+    for (int k = 1; k < 8; ++k) s += part[k][threadIdx.x & 31];
+    float *out = c < cols ? dgamma : dbeta;
+    if (out) out[c < cols ? c : c - cols] = (float)s;
+  }
+}
+
+// Rows per pass of a CTA and the layout over lanes for a number of vectors per row.
+int lanes_for(int vectors, int nv) {
+  int lanes = 1;
+  while (lanes * nv < vectors) lanes *= 2;
+  return lanes;
+}
+
+template <class T, int V, int NV, bool kBlock>
+int fwd(const LayerNormArgs &a, int lanes, int num_sms, cudaStream_t st) {
+  const int64_t groups = kBlock ? 1 : kNormThreads / lanes, want = (a.rows + groups - 1) / groups;
+  const int64_t most = (int64_t)num_sms * 6;
+  launch_chained(k_layer_norm_fwd<T, V, NV, kBlock>, (unsigned)(want < most ? want : most), kNormThreads, 0, st, a, lanes);
+  return 1;
+}
+int bwd_grid(int64_t rows, int groups) {
+  const int64_t want = (rows + groups - 1) / groups;
+  return (int)(want < kNormPartialRows ? want : kNormPartialRows);
+}
+template <class T, int V, int NV, bool kBlock>
+int bwd(const LayerNormArgs &a, int lanes, int num_sms, cudaStream_t st) {
+  int grid = bwd_grid(a.rows, kBlock ? 1 : kNormThreads / lanes);
+  const int most = num_sms * 3;
+  if (grid > most) grid = most;
+  if (!a.dgamma && !a.dbeta) {
+    launch_chained(k_layer_norm_bwd<T, V, NV, kBlock, false>, grid, kNormThreads, 0, st, a, lanes);
+    return 1;
+  }
+  launch_chained(k_layer_norm_bwd<T, V, NV, kBlock, true>, grid, kNormThreads, 0, st, a, lanes);
+  launch_chained(k_layer_norm_sums, (2 * a.cols + 31) / 32, 256, 0, st, (const float *)a.partials, grid, a.cols, a.dgamma, a.dbeta);
+  return 2;
+}
+
+bool vectors_fit(const void *p, int64_t ld, int64_t rows, int size) {
+  return !p || ((reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows <= 1 || (ld * size) % 16 == 0));
+}
+
+template <class T>
+int fwd_any(const LayerNormArgs &a, int num_sms, cudaStream_t st) {
+  constexpr int V = kVecOf<T>;
+  const bool vec = vectors_fit(a.x, a.ld_x, a.rows, sizeof(T)) && vectors_fit(a.y, a.ld_out, a.rows, sizeof(T));
+  const int n = vec ? (a.cols + V - 1) / V : a.cols;
+  if (vec) {
+    constexpr int most = 32 / V;                  // vectors of a lane that holds 32 elements
+    if (n <= 4) return fwd<T, V, 1, false>(a, lanes_for(n, 1), num_sms, st);
+    if (n <= 32 * 4) return fwd<T, V, 4, false>(a, lanes_for(n, 4), num_sms, st);
+    return fwd<T, V, most, true>(a, kNormThreads, num_sms, st);
+  }
+  if (n <= 4) return fwd<T, 1, 1, false>(a, lanes_for(n, 1), num_sms, st);
+  if (n <= 128) return fwd<T, 1, 4, false>(a, lanes_for(n, 4), num_sms, st);
+  if (n <= 2048) return fwd<T, 1, 8, true>(a, kNormThreads, num_sms, st);
+  return fwd<T, 1, 32, true>(a, kNormThreads, num_sms, st);
+}
+template <class T>
+int bwd_any(const LayerNormArgs &a, int num_sms, cudaStream_t st) {
+  constexpr int V = kVecOf<T>;
+  const bool vec = vectors_fit(a.x, a.ld_x, a.rows, sizeof(T)) && vectors_fit(a.dy, a.ld_dy, a.rows, sizeof(T)) &&
+                   vectors_fit(a.dx, a.ld_out, a.rows, sizeof(T));
+  const int n = vec ? (a.cols + V - 1) / V : a.cols;
+  if (vec) {
+    constexpr int few = 16 / V, most = 32 / V;    // vectors of a lane that holds 16 or 32 elements
+    if (n <= 4) return bwd<T, V, 1, false>(a, lanes_for(n, 1), num_sms, st);
+    if (n <= 32 * few) return bwd<T, V, few, false>(a, lanes_for(n, few), num_sms, st);
+    if (n <= kNormThreads) return bwd<T, V, 1, true>(a, kNormThreads, num_sms, st);
+    return bwd<T, V, most, true>(a, kNormThreads, num_sms, st);
+  }
+  if (n <= 4) return bwd<T, 1, 1, false>(a, lanes_for(n, 1), num_sms, st);
+  if (n <= 128) return bwd<T, 1, 4, false>(a, lanes_for(n, 4), num_sms, st);
+  if (n <= 2048) return bwd<T, 1, 8, true>(a, kNormThreads, num_sms, st);
+  return bwd<T, 1, 32, true>(a, kNormThreads, num_sms, st);
+}
+
+}  // namespace
+
+size_t layer_norm_partials(int64_t rows, int cols) { return (size_t)(rows < kNormPartialRows ? rows : kNormPartialRows) * 2 * (size_t)cols; }
+
+int launch_layer_norm_fwd(const LayerNormArgs &a, int num_sms, cudaStream_t st) {
+  if (a.dtype == GS_TYPE_F32) return fwd_any<float>(a, num_sms, st);
+  if (a.dtype == GS_TYPE_F16) return fwd_any<__half>(a, num_sms, st);
+  return fwd_any<__nv_bfloat16>(a, num_sms, st);
+}
+int launch_layer_norm_bwd(const LayerNormArgs &a, int num_sms, cudaStream_t st) {
+  if (a.dtype == GS_TYPE_F32) return bwd_any<float>(a, num_sms, st);
+  if (a.dtype == GS_TYPE_F16) return bwd_any<__half>(a, num_sms, st);
+  return bwd_any<__nv_bfloat16>(a, num_sms, st);
+}
+
+}  // namespace gs
