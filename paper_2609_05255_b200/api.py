@@ -513,14 +513,10 @@ class AdamTensor:
         self._more = (_vp * max(1, len(self.more_grads)))(*[_ptr(g) for g in self.more_grads])
 
     def c_struct(self) -> GsAdamTensor:
-        t = GsAdamTensor()
-        t.param, t.grad, t.exp_avg, t.exp_avg_sq = _ptr(self.param), _ptr(self.grad), _ptr(self.exp_avg), _ptr(self.exp_avg_sq)
-        t.half_copy = _ptr(self.half_copy)
-        t.rows, t.cols, t.lr = self.rows, self.cols, C.cast(self.lr, C.POINTER(C.c_float))
-        t.beta1, t.beta2, t.eps = self.beta1, self.beta2, self.eps
-        t.more_grads = C.cast(self._more, C.POINTER(_vp)) if self.more_grads else None
-        t.num_more_grads = len(self.more_grads)
-        return t
+        more = C.cast(self._more, C.POINTER(_vp)) if self.more_grads else None
+        return GsAdamTensor(_ptr(self.param), _ptr(self.grad), _ptr(self.exp_avg), _ptr(self.exp_avg_sq), _ptr(self.half_copy),
+                            self.rows, self.cols, C.cast(self.lr, C.POINTER(C.c_float)), self.beta1, self.beta2, self.eps,
+                            more, len(self.more_grads))
 
 
 def gs_adam_step(ctx: Context, tensors, step: int, stream=None) -> None:
@@ -579,7 +575,7 @@ def _matrix(ctx: Context, t: Optional[torch.Tensor], name: str, rows: int, cols:
     """(address, elements from row to row) of a [rows, cols] tensor whose rows are contiguous."""
     if t is None:
         return None, 0
-    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.device != ctx.device:
+    if t.dtype is not dtype or t.shape != (rows, cols) or t.device != ctx.device:
         _invalid(f"{name} must be a {dtype} tensor [{rows}, {cols}] on {ctx.device}, got {t.dtype} {list(t.shape)} on {t.device}")
     ld, one = t.stride()
     if one != 1 and cols > 1:

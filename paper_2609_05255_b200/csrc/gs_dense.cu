@@ -28,6 +28,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "gs_device.cuh"
 
 namespace gs {
@@ -41,10 +43,10 @@ constexpr int kRows = 128;                    // rows of a tile of k_dense_rows,
 constexpr int kStep = 64;                     // columns (k_dense_rows) or rows (k_dense_weights) of a pipeline step
 constexpr uint32_t kTileBytes = kRows * tma::kRowBytes;       // 128 x 64 values
 constexpr uint32_t kBoxBytes = kStep * tma::kRowBytes;        // 64 x 64 values
-constexpr int kMaxStages = 8;
+constexpr int kMaxStages = 12;
 constexpr uint32_t kSmemMost = 232448;        // 227 KB
 
-enum { kWarpLoad = 0, kWarpMma = 1, kWarpResidual = 2, kWarpEpilogue = 4, kWarpTransform = 8 };
+enum { kWarpLoad = 0, kWarpMma = 1, kWarpResidual = 2, kWarpEpilogue = 4 };
 constexpr int kTransformThreads = 256;
 enum { kWarpWorker = 4, kWorkerWarps = 8 };   // of k_dense_weights, behind the warps that load and issue
 
@@ -53,22 +55,48 @@ __device__ __forceinline__ float rcp_approx(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float logistic(float x) { return rcp_approx(1.f + ex2_approx(-1.4426950408889634f * x)); }
-// gelu(z) = z logistic(2 sqrt(2 / pi) (z + 0.044715 z^3)), the tanh form
-__device__ __forceinline__ float gelu_arg(float z) { return z * fmaf(0.07135481627159806f, z * z, 1.5957691216057308f); }
-__device__ __forceinline__ float activate(int act, float z) {
-  if (act == GS_DENSE_RELU) return z < 0.f ? 0.f : z;      // (a NaN stays)
-  if (act == GS_DENSE_SILU) return z * logistic(z);
-  if (act == GS_DENSE_GELU) return z * logistic(gelu_arg(z));
-  return z;
+// logistic(x) of two values, from -log2(e) x
+__device__ __forceinline__ float2 logistic2(float2 t) {
+  t = add2(make_float2(ex2_approx(t.x), ex2_approx(t.y)), both(1.f));
+  return make_float2(rcp_approx(t.x), rcp_approx(t.y));
 }
-// act' of the smooth ones.  Beyond |z| = 128 it is 1 or 0 in fp32; the clamp keeps z^3 finite (and a NaN a NaN).
-__device__ __forceinline__ float activate_grad(int act, float z) {
-  z = z > 128.f ? 128.f : z < -128.f ? -128.f : z;
-  const float gelu = act == GS_DENSE_GELU ? 1.f : 0.f;
-  const float p = logistic(act == GS_DENSE_GELU ? gelu_arg(z) : z);
-  const float slope = fmaf(gelu, fmaf(0.21406444881479418f, z * z, 0.5957691216057308f), 1.f);     // of the logistic's argument
-  return fmaf(z * p * (1.f - p), slope, p);
+constexpr float kMinusLog2e = -1.4426950408889634f;
+// gelu(z) = z logistic(u), u = 2 sqrt(2 / pi) (z + 0.044715 z^3): the tanh form.  -log2(e) u:
+__device__ __forceinline__ float2 gelu_arg2(float2 z, float2 zz) {
+  return mul2(z, fma2(zz, both(0.07135481627159806f * kMinusLog2e), both(1.5957691216057308f * kMinusLog2e)));
+}
+template <int kAct>
+__device__ __forceinline__ void activate8(float2 z[4]) {
+  if constexpr (kAct == GS_DENSE_RELU) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = make_float2(z[i].x < 0.f ? 0.f : z[i].x, z[i].y < 0.f ? 0.f : z[i].y);      // (a NaN stays)
+  } else if constexpr (kAct == GS_DENSE_SILU) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = mul2(z[i], logistic2(mul2(z[i], both(kMinusLog2e))));
+  } else if constexpr (kAct == GS_DENSE_GELU) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = mul2(z[i], logistic2(gelu_arg2(z[i], mul2(z[i], z[i]))));
+  }
+}
+// act' of the smooth ones: p + z p (1 - p) u'.  Beyond |z| = 128 gelu' is 1 or 0 in fp32; the clamp keeps z^3 finite (and a NaN a
+// NaN).  Silu needs none: p (1 - p) is 0 before z overflows.
+template <int kAct>
+__device__ __forceinline__ void activate_grad8(float2 z[4]) {
+  if constexpr (kAct == GS_DENSE_SILU) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 p = logistic2(mul2(z[i], both(kMinusLog2e)));
+      z[i] = fma2(z[i], fma2(make_float2(-p.x, -p.y), p, p), p);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      z[i].x = z[i].x > 128.f ? 128.f : z[i].x < -128.f ? -128.f : z[i].x;
+      z[i].y = z[i].y > 128.f ? 128.f : z[i].y < -128.f ? -128.f : z[i].y;
+      const float2 zz = mul2(z[i], z[i]), p = logistic2(gelu_arg2(z[i], zz));
+      z[i] = fma2(mul2(z[i], fma2(make_float2(-p.x, -p.y), p, p)), fma2(zz, both(0.21406444881479418f), both(1.5957691216057308f)), p);
+    }
+  }
 }
 
 // Shared-memory matrix descriptors for the 128-byte swizzle.  K-major (a row holds 64 elements of the contraction): groups of
@@ -101,34 +129,44 @@ __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("
 
 // dz of eight values: part 0 high, then what is left; in place of dy (a), preact (b) and at c.
 // kParts: 1 ReLU, 2 or 3 smooth; kScale: the second part times 2^11.  dz itself is added to sums where there are any.
-template <class T, int kParts, bool kScale, bool kSums>
-__device__ __forceinline__ void transform_chunk(unsigned char *a, unsigned char *b, unsigned char *c, int act, float *sums) {
-  uint4 dy = *reinterpret_cast<const uint4 *>(a), z = *reinterpret_cast<const uint4 *>(b), third = make_uint4(0u, 0u, 0u, 0u);
+template <class T, int kAct, int kParts, bool kScale, bool kSums>
+__device__ __forceinline__ void transform_chunk(unsigned char *a, unsigned char *b, unsigned char *c, uint4 dy, uint4 z, float2 *sums) {
+  uint4 third;
   uint32_t *dw = &dy.x, *zw = &z.x, *tw = &third.x;
+  float2 g[4];
+  unpack<T>(z, &g[0].x);
+  if constexpr (kParts > 1) activate_grad8<kAct>(g);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float2 d = widen2<T>(dw[i]), p = widen2<T>(zw[i]);
-    if (kParts == 1) {
-      const float2 v = make_float2(p.x > 0.f ? d.x : 0.f, p.y > 0.f ? d.y : 0.f);
-      dw[i] = narrow2<T>(v.x, v.y);
-      if (kSums) { sums[2 * i] += v.x; sums[2 * i + 1] += v.y; }
-    } else {
-      float2 v = make_float2(d.x * activate_grad(act, p.x), d.y * activate_grad(act, p.y));
-      if (kSums) { sums[2 * i] += v.x; sums[2 * i + 1] += v.y; }
-      dw[i] = narrow2<T>(v.x, v.y);
-      float2 f = widen2<T>(dw[i]);
-      v.x -= f.x; v.y -= f.y;
-      zw[i] = kScale ? narrow2<T>(v.x * 2048.f, v.y * 2048.f) : narrow2<T>(v.x, v.y);
-      if (kParts == 3) {
-        f = widen2<T>(zw[i]);
-        tw[i] = narrow2<T>(v.x - f.x, v.y - f.y);
-      }
+    const float2 d = widen2<T>(dw[i]);
+    float2 v = kParts == 1 ? make_float2(g[i].x > 0.f ? d.x : 0.f, g[i].y > 0.f ? d.y : 0.f) : mul2(d, g[i]);
+    if (kSums) sums[i] = add2(sums[i], v);
+    dw[i] = narrow2<T>(v.x, v.y);
+    if (kParts >= 2) {
+      v = fma2(widen2<T>(dw[i]), both(-1.f), v);
+      if (kScale) v = mul2(v, both(2048.f));
+      zw[i] = narrow2<T>(v.x, v.y);
+    }
+    if (kParts == 3) {
+      v = fma2(widen2<T>(zw[i]), both(-1.f), v);
+      tw[i] = narrow2<T>(v.x, v.y);
     }
   }
   *reinterpret_cast<uint4 *>(a) = dy;
   if (kParts >= 2) *reinterpret_cast<uint4 *>(b) = z;
   if (kParts == 3) *reinterpret_cast<uint4 *>(c) = third;
 }
+__device__ __forceinline__ uint4 shared16(const unsigned char *p) { return *reinterpret_cast<const uint4 *>(p); }
+
+// A place in a ring of stages and the parity of the passes over it, moved on without divisions: what one thread does for a step
+// (wait, descriptors, four MMAs, commit) is a chain of dependent instructions, and at 650 cycles a step it was the bound (20 011
+// rows of 1024 to 1024 in 56 us instead of 48).
+struct Ring {
+  uint32_t s = 0, parity = 0;
+  __device__ __forceinline__ void next(uint32_t stages) {
+    if (++s == stages) { s = 0; parity ^= 1u; }
+  }
+};
 
 struct RowsArgs {
   CUtensorMap a, z, b, out, keep, residual;     // x or dy; preact (backward); W; y or dx; preact (forward); residual
@@ -139,41 +177,54 @@ struct RowsArgs {
   int out_cols, m_tiles, n_tiles, k_blocks, k;   // k: length of the contraction
   int bn;                                       // columns of a tile, at most 256
   uint32_t b_bytes;                             // of one step's weights
-  int stages, resident, staging;                // staging: tiles per output on their way out, 1 or 2
-  int act, has_keep, has_residual;
+  int stages, resident;
+  int out_slots, keep_slots;                    // tiles of y (where the residual arrives) and preact on their way out: 2 or 4
+  int has_keep, has_residual;
   uint32_t tmem_cols;
   unsigned long long *timeout;
 };
 
 struct RowsBarriers {
-  uint64_t full[kMaxStages], ready[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], res_full[2], res_empty[2], weights, drained;
-  uint32_t tmem, dead, ok, pad;
+  uint64_t full[kMaxStages], ready[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], res_full[4], res_empty[4], weights, drained;
+  uint32_t tmem, dead, ok[2];
 };
 
+// Warps that take tiles out: two groups, which take chunks of 64 columns in turn, so that one computes while the other waits at its
+// barriers.  In the forward, whose activation is the work, a group has eight warps, two for each 32 lanes of tensor memory.
+// (One group of four: 943 us instead of 507, and 319 with the residual landing where y leaves, for 1M rows of 256 to 256 in bf16
+// with SiLU, residual and kept pre-activation.)
+template <bool kForward> constexpr int kGroupWarps = kForward ? 8 : 4;
+template <bool kForward, int kParts> constexpr int kRowsThreads = 32 * (kWarpEpilogue + 2 * kGroupWarps<kForward>) + (kParts ? kTransformThreads : 0);
+
 // kForward: B is W [out, in], K-major, and the epilogue has bias, activation, residual and kept pre-activation.  Else B is W
-// [contraction, out], MN-major, A is dz in kParts parts (0: dy as it is).
-template <class T, bool kForward, int kParts>
-__global__ void __launch_bounds__(kParts ? 512 : 256, 1) k_dense_rows(const __grid_constant__ RowsArgs a) {
+// [contraction, out], MN-major, A is dz in kParts parts (0: dy as it is).  (The activation is the kernel's: chosen inside, between
+// two unrolled bodies, it kept the values from overlapping.)
+template <bool kForward, int kAct> constexpr int kRowsParts = kForward || kAct == GS_DENSE_NONE ? 0 : kAct == GS_DENSE_RELU ? 1 : 2;
+template <class T, bool kForward, int kAct>
+__global__ void __launch_bounds__((kRowsThreads<kForward, kRowsParts<kForward, kAct>>), 1) k_dense_rows(const __grid_constant__ RowsArgs a) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char *smem = smem_raw + ((1024u - (tc::smem_addr(smem_raw) & 1023u)) & 1023u);
+  constexpr int kParts = kRowsParts<kForward, kAct>;
   constexpr uint32_t kStageA = kParts ? 2 * kTileBytes : kTileBytes;
   const uint32_t stage_bytes = kStageA + (a.resident ? 0u : a.b_bytes);
   unsigned char *stages = smem + (a.resident ? (uint32_t)a.k_blocks * a.b_bytes : 0u);
   unsigned char *out_tiles = stages + (uint32_t)a.stages * stage_bytes;
-  unsigned char *keep_tiles = out_tiles + (uint32_t)a.staging * kTileBytes;
-  unsigned char *res_tiles = keep_tiles + (a.has_keep ? (uint32_t)a.staging * kTileBytes : 0u);
-  float *bias = reinterpret_cast<float *>(res_tiles + (a.has_residual ? (uint32_t)a.staging * kTileBytes : 0u));
+  unsigned char *keep_tiles = out_tiles + (uint32_t)a.out_slots * kTileBytes;
+  float *bias = reinterpret_cast<float *>(keep_tiles + (uint32_t)a.keep_slots * kTileBytes);
   RowsBarriers &bars = *reinterpret_cast<RowsBarriers *>(bias + 256);
   volatile uint32_t *dead = &bars.dead;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int kGroup = kGroupWarps<kForward>, kWarpTransform = kWarpEpilogue + 2 * kGroup;
   auto bar = [](const uint64_t &b) { return tc::smem_addr(&b); };
+  const int n_tile = blockIdx.x % a.n_tiles, n0 = n_tile * a.bn;
+  const int m_first = blockIdx.x / a.n_tiles, m_step = gridDim.x / a.n_tiles;
+  const uint32_t acc_cols = (uint32_t)(a.bn + 63) & ~63u;
+  const int chunks = (min(a.bn, a.out_cols - n0) + 63) / 64;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < a.stages; ++s) { tma::init(bar(bars.full[s]), 1); tma::init(bar(bars.ready[s]), kTransformThreads / 32); tma::init(bar(bars.empty[s]), 1); }
-    for (int i = 0; i < 2; ++i) {
-      tma::init(bar(bars.acc_full[i]), 1); tma::init(bar(bars.acc_empty[i]), 4);
-      tma::init(bar(bars.res_full[i]), 1); tma::init(bar(bars.res_empty[i]), 1);
-    }
+    for (int i = 0; i < 2; ++i) { tma::init(bar(bars.acc_full[i]), 1); tma::init(bar(bars.acc_empty[i]), chunks * kGroup); }
+    for (int i = 0; i < 4; ++i) { tma::init(bar(bars.res_full[i]), 1); tma::init(bar(bars.res_empty[i]), 1); }
     tma::init(bar(bars.weights), 1); tma::init(bar(bars.drained), 1);
     bars.dead = 0u;
     tc::fence_barrier_init();
@@ -184,11 +235,6 @@ __global__ void __launch_bounds__(kParts ? 512 : 256, 1) k_dense_rows(const __gr
   tc::fence_after_sync();
   const uint32_t tmem = bars.tmem;
   dependency_wait();
-
-  const int n_tile = blockIdx.x % a.n_tiles, n0 = n_tile * a.bn;
-  const int m_first = blockIdx.x / a.n_tiles, m_step = gridDim.x / a.n_tiles;
-  const uint32_t acc_cols = (uint32_t)(a.bn + 63) & ~63u;
-  const int chunks = (min(a.bn, a.out_cols - n0) + 63) / 64;
 
   if (warp == kWarpLoad) {
     if (lane == 0) {
@@ -201,12 +247,13 @@ __global__ void __launch_bounds__(kParts ? 512 : 256, 1) k_dense_rows(const __gr
         for (int kb = 0; kb < a.k_blocks; ++kb) load_weights(tc::smem_addr(smem) + kb * a.b_bytes, kb, bar(bars.weights));
       }
       uint32_t it = 0;
+      Ring at;
       bool ok = true;
+      const uint32_t dst0 = tc::smem_addr(stages), full0 = bar(bars.full[0]), empty0 = bar(bars.empty[0]);
       for (int m = m_first; ok && m < a.m_tiles; m += m_step)
-        for (int kb = 0; kb < a.k_blocks; ++kb, ++it) {
-          const uint32_t s = it % a.stages;
-          if (!(ok = tma::wait(bar(bars.empty[s]), (it / a.stages & 1u) ^ 1u, dead))) break;
-          const uint32_t dst = tc::smem_addr(stages) + s * stage_bytes, f = bar(bars.full[s]);
+        for (int kb = 0; kb < a.k_blocks; ++kb, ++it, at.next(a.stages)) {
+          if (!(ok = tma::wait(empty0 + at.s * 8, at.parity ^ 1u, dead))) break;
+          const uint32_t dst = dst0 + at.s * stage_bytes, f = full0 + at.s * 8;
           tma::expect(f, stage_bytes);
           tma::load(dst, &a.a, kb * kStep, m * kRows, f);
           if (kParts) tma::load(dst + kTileBytes, &a.z, kb * kStep, m * kRows, f);
@@ -214,143 +261,170 @@ __global__ void __launch_bounds__(kParts ? 512 : 256, 1) k_dense_rows(const __gr
         }
       if (!ok) {                          // copies in flight land before the CTA leaves
         for (uint32_t k = it > (uint32_t)a.stages ? it - a.stages : 0u; k < it; ++k)
-          for (int t = 0; t < (1 << 16) && !tma::try_wait(bar(bars.full[k % a.stages]), k / a.stages & 1u); ++t) {}
+          tma::settle(bar(bars.full[k % a.stages]), k / a.stages & 1u);
       }
       if (a.resident)
-        for (int t = 0; t < (1 << 20) && !tma::try_wait(bar(bars.weights), 0u); ++t) {}
+        tma::settle(bar(bars.weights), 0u);
     }
   } else if (warp == kWarpMma) {
     if (lane == 0) {
       const uint32_t desc = idesc_of<T>((a.bn + 15) & ~15, false, !kForward);
-      uint32_t it = 0, tile = 0;
+      // descriptors of the first stage and of the first step's weights; further on is an addition (in 16 bytes) to the address field
+      constexpr uint64_t kNextB = kForward ? 2 : 128;
+      const uint64_t a_desc = desc_swizzled(tc::smem_addr(stages), 16), stage16 = stage_bytes >> 4, b16 = a.resident ? a.b_bytes >> 4 : 0u;
+      const uint64_t b_desc = desc_swizzled(a.resident ? tc::smem_addr(smem) : tc::smem_addr(stages) + kStageA, kForward ? 16 : kBoxBytes);
+      const uint32_t ready0 = kParts ? bar(bars.ready[0]) : bar(bars.full[0]), empty0 = bar(bars.empty[0]);
+      const int last_steps = (a.k - (a.k_blocks - 1) * kStep + 15) / 16;
+      uint32_t tile = 0;
+      Ring at;
       bool ok = !a.resident || m_first >= a.m_tiles || tma::wait(bar(bars.weights), 0u, dead);
       for (int m = m_first; ok && m < a.m_tiles; m += m_step, ++tile) {
         const uint32_t buf = tile & 1u;
         if (!(ok = tma::wait(bar(bars.acc_empty[buf]), (tile >> 1 & 1u) ^ 1u, dead))) break;
-        tc::fence_after_sync();
         const uint32_t d = tmem + buf * acc_cols;
-        for (int kb = 0; kb < a.k_blocks; ++kb, ++it) {
-          const uint32_t s = it % a.stages;
-          if (!(ok = tma::wait(kParts ? bar(bars.ready[s]) : bar(bars.full[s]), it / a.stages & 1u, dead))) break;
+        for (int kb = 0; kb < a.k_blocks; ++kb, at.next(a.stages)) {
+          const uint64_t da = a_desc + at.s * stage16, db = b_desc + (a.resident ? kb * b16 : at.s * stage16);
+          if (!(ok = tma::wait(ready0 + at.s * 8, at.parity, dead))) break;
           tc::fence_after_sync();
-          const uint32_t A = tc::smem_addr(stages) + s * stage_bytes;
-          const uint32_t B = a.resident ? tc::smem_addr(smem) + kb * a.b_bytes : A + kStageA;
-          const int steps = min(4, (a.k - kb * kStep + 15) / 16);
+          const int steps = kb == a.k_blocks - 1 ? last_steps : 4;
 #pragma unroll
           for (int p = 0; p < (kParts == 2 ? 2 : 1); ++p)
-            for (int ks = 0; ks < steps; ++ks)
-              tc::mma(d, desc_swizzled(A + p * kTileBytes + ks * 32, 16), kForward ? desc_swizzled(B + ks * 32, 16) : desc_swizzled(B + ks * 2048, kBoxBytes),
-                      (kb | p | ks) ? 1u : 0u, desc);
-          tc::commit(bar(bars.empty[s]));
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              if (ks < steps) tc::mma(d, da + p * (kTileBytes >> 4) + ks * 2, db + ks * kNextB, p || ks ? 1u : (uint32_t)kb, desc);
+          tc::commit(empty0 + at.s * 8);
         }
         if (ok) tc::commit(bar(bars.acc_full[buf]));
       }
       // products in flight end before tensor memory is given back
       tc::commit(bar(bars.drained));
-      for (int t = 0; t < (1 << 20) && !tma::try_wait(bar(bars.drained), 0u); ++t) {}
+      tma::settle(bar(bars.drained), 0u);
     }
   } else if (kForward && warp == kWarpResidual) {
     if (lane == 0 && a.has_residual) {
       uint32_t it = 0;
+      Ring at;
       bool ok = true;
       for (int m = m_first; ok && m < a.m_tiles; m += m_step)
-        for (int c = 0; c < chunks; ++c, ++it) {
-          const uint32_t s = it % a.staging;
-          if (!(ok = tma::wait(bar(bars.res_empty[s]), (it / a.staging & 1u) ^ 1u, dead))) break;
+        for (int c = 0; c < chunks; ++c, ++it, at.next(a.out_slots)) {
+          const uint32_t s = at.s;
+          if (!(ok = tma::wait(bar(bars.res_empty[s]), at.parity ^ 1u, dead))) break;
           tma::expect(bar(bars.res_full[s]), kTileBytes);
-          tma::load(tc::smem_addr(res_tiles) + s * kTileBytes, &a.residual, n0 + c * 64, m * kRows, bar(bars.res_full[s]));
+          tma::load(tc::smem_addr(out_tiles) + s * kTileBytes, &a.residual, n0 + c * 64, m * kRows, bar(bars.res_full[s]));
         }
       if (!ok)
-        for (uint32_t k = it > (uint32_t)a.staging ? it - a.staging : 0u; k < it; ++k)
-          for (int t = 0; t < (1 << 16) && !tma::try_wait(bar(bars.res_full[k % a.staging]), k / a.staging & 1u); ++t) {}
+        for (uint32_t k = it > (uint32_t)a.out_slots ? it - a.out_slots : 0u; k < it; ++k)
+          tma::settle(bar(bars.res_full[k % a.out_slots]), k / a.out_slots & 1u);
     }
   } else if (warp >= kWarpEpilogue && warp < kWarpTransform) {
-    const int tid = threadIdx.x - kWarpEpilogue * 32;              // = lane of tensor memory = row of the tile
-    if (kForward)
-      for (int c = tid; c < 256; c += 128) bias[c] = a.bias && c < a.bn && n0 + c < a.out_cols ? __ldg(a.bias + n0 + c) : 0.f;
+    const int group = (warp - kWarpEpilogue) / kGroup, tid = threadIdx.x - (kWarpEpilogue + group * kGroup) * 32;
+    const int row = tid & 127;                                     // of the tile = lane of tensor memory
+    const int threads = kGroup * 32;
+    if (kForward) {
+      if (group == 0 && tid < 256) bias[tid] = a.bias && tid < a.bn && n0 + tid < a.out_cols ? __ldg(a.bias + n0 + tid) : 0.f;
+      named_sync(3, 2 * threads);
+    }
     // A copy out of shared memory writes whole 16-byte chunks: the columns behind the last multiple of 8 go one by one.
     const int tail = a.out_cols & 7, whole = a.out_cols - tail;
     auto store_tail = [&](void *rows, int64_t ld, int m, const float *w) {
-      const int row = m * kRows + tid;
-      if (row >= a.rows) return;
-      T *p = static_cast<T *>(rows) + (int64_t)row * ld + whole;
+      const int r = m * kRows + row;
+      if (r >= a.rows) return;
+      T *p = static_cast<T *>(rows) + (int64_t)r * ld + whole;
 #pragma unroll
       for (int i = 0; i < 7; ++i)
         if (i < tail) p[i] = narrow<T>(w[i]);
     };
-    uint32_t it = 0, tile = 0;
+    const bool behind = a.out_slots == 4 && a.keep_slots != 2;     // a group's last copies may still read while it fills the other slots
+    uint32_t tile = 0, before = 4;
+    Ring at;
     bool ok = true;
     for (int m = m_first; ok && m < a.m_tiles; m += m_step, ++tile) {
       const uint32_t buf = tile & 1u;
-      for (int c = 0; c < chunks; ++c, ++it) {
-        const uint32_t s = it % a.staging;
+      for (int c = 0; c < chunks; ++c, at.next(a.out_slots)) {
+        const uint32_t s = at.s;
+        if ((int)(s & 1u) != group) continue;
         if (tid == 0) {
-          bool all = c > 0 || tma::wait(bar(bars.acc_full[buf]), tile >> 1 & 1u, dead);
-          if (kForward && a.has_residual) all = all && tma::wait(bar(bars.res_full[s]), it / a.staging & 1u, dead);
-          if (a.staging == 2) tma::stores_read<1>(); else tma::stores_read<0>();
-          bars.ok = all ? 1u : 0u;
+          if (kForward && a.has_residual) {                        // the slot before is free for the residual of a chunk to come
+            tma::stores_read<0>();
+            if (before < 4) tma::arrive(bar(bars.res_empty[before]));
+            before = s;
+          } else if (behind) {
+            tma::stores_read<1>();
+          } else {
+            tma::stores_read<0>();
+          }
+          bool all = tma::wait(bar(bars.acc_full[buf]), tile >> 1 & 1u, dead);
+          if (kForward && a.has_residual) all = all && tma::wait(bar(bars.res_full[s]), at.parity, dead);
+          bars.ok[group] = all ? 1u : 0u;
         }
-        named_sync(1, 128);
-        if (!(ok = *(volatile uint32_t *)&bars.ok != 0u)) break;
+        named_sync(1 + group, threads);
+        if (!(ok = *(volatile uint32_t *)&bars.ok[group] != 0u)) break;
         tc::fence_after_sync();
-        unsigned char *out = out_tiles + s * kTileBytes + tid * tma::kRowBytes, *keep = keep_tiles + s * kTileBytes + tid * tma::kRowBytes;
-        const unsigned char *res = res_tiles + s * kTileBytes + tid * tma::kRowBytes;
+        const uint32_t ks = a.keep_slots == 4 ? s : (uint32_t)group;
+        unsigned char *out = out_tiles + s * kTileBytes + row * tma::kRowBytes, *keep = keep_tiles + ks * kTileBytes + row * tma::kRowBytes;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float v[32];
-          load32(tmem + buf * acc_cols + c * 64 + h * 32 + ((uint32_t)(tid & 96) << 16), v);
+        for (int half = 0; half < (kGroup == 8 ? 1 : 2); ++half) {
+          const int h = kGroup == 8 ? tid >> 7 : half;
+          float2 v[16];
+          load32(tmem + buf * acc_cols + c * 64 + h * 32 + ((uint32_t)(tid & 96) << 16), &v[0].x);
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const uint32_t at = (uint32_t)((h * 4 + q) ^ (tid & 7)) * 16u;
-            float *w = v + q * 8;
+            const uint32_t in = (uint32_t)((h * 4 + q) ^ (row & 7)) * 16u;
+            const int col = c * 64 + h * 32 + q * 8;
+            float2 *w = v + q * 4;
             if (kForward) {
-              const float4 b0 = *reinterpret_cast<const float4 *>(bias + c * 64 + h * 32 + q * 8), b1 = *reinterpret_cast<const float4 *>(bias + c * 64 + h * 32 + q * 8 + 4);
-              w[0] += b0.x; w[1] += b0.y; w[2] += b0.z; w[3] += b0.w;
-              w[4] += b1.x; w[5] += b1.y; w[6] += b1.z; w[7] += b1.w;
+              const float4 b0 = *reinterpret_cast<const float4 *>(bias + col), b1 = *reinterpret_cast<const float4 *>(bias + col + 4);
+              w[0] = add2(w[0], make_float2(b0.x, b0.y)); w[1] = add2(w[1], make_float2(b0.z, b0.w));
+              w[2] = add2(w[2], make_float2(b1.x, b1.y)); w[3] = add2(w[3], make_float2(b1.z, b1.w));
               if (a.has_keep) {
-                *reinterpret_cast<uint4 *>(keep + at) = pack<T>(w);
-                if (tail && n0 + c * 64 + h * 32 + q * 8 == whole) store_tail(a.keep_rows, a.ld_keep, m, w);
+                *reinterpret_cast<uint4 *>(keep + in) = pack<T>(&w[0].x);
+                if (tail && n0 + col == whole) store_tail(a.keep_rows, a.ld_keep, m, &w[0].x);
               }
-#pragma unroll
-              for (int i = 0; i < 8; ++i) w[i] = activate(a.act, w[i]);
+              activate8<kAct>(w);
               if (a.has_residual) {
-                float r[8];
-                unpack<T>(*reinterpret_cast<const uint4 *>(res + at), r);
+                float2 r[4];
+                unpack<T>(*reinterpret_cast<const uint4 *>(out + in), &r[0].x);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] += r[i];
+                for (int i = 0; i < 4; ++i) w[i] = add2(w[i], r[i]);
               }
             }
-            *reinterpret_cast<uint4 *>(out + at) = pack<T>(w);
-            if (tail && n0 + c * 64 + h * 32 + q * 8 == whole) store_tail(a.out_rows, a.ld_out, m, w);
+            *reinterpret_cast<uint4 *>(out + in) = pack<T>(&w[0].x);
+            if (tail && n0 + col == whole) store_tail(a.out_rows, a.ld_out, m, &w[0].x);
           }
         }
         tc::fence_before_sync();
         tc::fence_generic_writes();
-        if (c == chunks - 1 && lane == 0) tma::arrive(bar(bars.acc_empty[buf]));
-        named_sync(1, 128);
+        if (lane == 0) tma::arrive(bar(bars.acc_empty[buf]));
+        named_sync(1 + group, threads);
         if (tid == 0) {
           const bool any = n0 + c * 64 < whole;
           if (any) tma::store(&a.out, n0 + c * 64, m * kRows, tc::smem_addr(out_tiles) + s * kTileBytes);
-          if (kForward && a.has_keep && any) tma::store(&a.keep, n0 + c * 64, m * kRows, tc::smem_addr(keep_tiles) + s * kTileBytes);
+          if (kForward && a.has_keep && any) tma::store(&a.keep, n0 + c * 64, m * kRows, tc::smem_addr(keep_tiles) + ks * kTileBytes);
           tma::store_commit();
-          if (kForward && a.has_residual) tma::arrive(bar(bars.res_empty[s]));
         }
       }
     }
     if (tid == 0) tma::stores_done();
   } else if (kParts && warp >= kWarpTransform) {
     const int t = threadIdx.x - kWarpTransform * 32;
-    uint32_t it = 0;
+    Ring at;
     bool ok = true;
     for (int m = m_first; ok && m < a.m_tiles; m += m_step)
-      for (int kb = 0; kb < a.k_blocks; ++kb, ++it) {
-        const uint32_t s = it % a.stages;
-        if (!(ok = __all_sync(0xffffffffu, tma::wait(bar(bars.full[s]), it / a.stages & 1u, dead)))) break;
+      for (int kb = 0; kb < a.k_blocks; ++kb, at.next(a.stages)) {
+        const uint32_t s = at.s;
+        if (!(ok = __all_sync(0xffffffffu, tma::wait(bar(bars.full[s]), at.parity, dead)))) break;
         unsigned char *A = stages + s * stage_bytes;
+        constexpr int kChunks = (int)(kTileBytes / 16 / kTransformThreads);
+        uint4 dy[kChunks], z[kChunks];
 #pragma unroll
-        for (int u = 0; u < (int)(kTileBytes / 16 / kTransformThreads); ++u) {
-          const uint32_t at = (uint32_t)(u * kTransformThreads + t) * 16u;
-          transform_chunk<T, kParts, false, false>(A + at, A + kTileBytes + at, nullptr, a.act, nullptr);
+        for (int u = 0; u < kChunks; ++u) {
+          dy[u] = shared16(A + (u * kTransformThreads + t) * 16);
+          z[u] = shared16(A + kTileBytes + (u * kTransformThreads + t) * 16);
+        }
+#pragma unroll
+        for (int u = 0; u < kChunks; ++u) {
+          unsigned char *p = A + (u * kTransformThreads + t) * 16;
+          transform_chunk<T, kAct, kParts, false, false>(p, p + kTileBytes, nullptr, dy[u], z[u], nullptr);
         }
         tc::fence_generic_writes();
         __syncwarp();
@@ -370,32 +444,39 @@ struct WeightsArgs {
   CUtensorMap dy, z, x;
   int n, k, n_tiles, k_tiles, splits, row_blocks;
   int bk;                         // columns of x of a tile, at most 256
-  int stages, act, want_db;
+  int stages, want_db;
   int ld;                         // row length of the partial sums
   float *partials, *db_partials;  // [splits, n, ld], [splits, n]
   uint32_t tmem_cols;
   unsigned long long *timeout;
 };
-constexpr int kFlush = 8;                       // steps of 64 rows after which an accumulator is emptied
+constexpr int kWStep = 64;                      // rows of a step (32: 221 us instead of 173 without activation)
+constexpr uint32_t kWBoxBytes = kWStep * tma::kRowBytes;
+constexpr int kFlush = 8;                       // steps after which an accumulator is emptied
 struct WeightsBarriers {
   uint64_t full[kMaxStages], ready[kMaxStages], empty[kMaxStages], sum_full[2], sum_empty[2], done;
   uint32_t tmem, dead, pad[2];
 };
 
-// kParts: 0 dy is dz; 1 ReLU; 2 and 3 smooth activations in so many parts.  kScale: what is left lies 2^11 higher.
+// Parts of dz: 0 it is dy; 1 ReLU; 2 (fp16, what is left lies 2^11 higher) and 3 (bf16) smooth activations.
+template <class T>
+__host__ __device__ constexpr int weight_parts(int act) {
+  return act == GS_DENSE_NONE ? 0 : act == GS_DENSE_RELU ? 1 : __is_same(T, __half) ? 2 : 3;
+}
 //
 // The tensor core cuts off what an addition leaves below the accumulator's last bit, so over thousands of additions the sums
 // shrink: 1M rows in 74 splits were 9e-5 off.  So the accumulator of dz, or of its high part, is emptied every 8 steps, after
 // 32 additions, into fp32 registers of the eight worker warps, which round to nearest (two accumulators in turn where there
 // is one part: 4e-7 off).  The other parts have an accumulator of their own, which loses as much of 2^-8 as much.
-template <class T, int kParts, bool kScale>
+template <class T, int kAct>
 __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant__ WeightsArgs a) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char *smem = smem_raw + ((1024u - (tc::smem_addr(smem_raw) & 1023u)) & 1023u);
-  constexpr bool kLow = kParts >= 2;
-  constexpr uint32_t kStageA = (kParts == 3 ? 3 : kParts ? 2 : 1) * 2 * kBoxBytes;
+  constexpr int kParts = weight_parts<T>(kAct);
+  constexpr bool kLow = kParts >= 2, kScale = kParts == 2;
+  constexpr uint32_t kStageA = (kParts == 3 ? 3 : kParts ? 2 : 1) * 2 * kWBoxBytes;
   const int x_boxes = (a.bk + 63) / 64;
-  const uint32_t stage_bytes = kStageA + x_boxes * kBoxBytes;
+  const uint32_t stage_bytes = kStageA + x_boxes * kWBoxBytes;
   float *sums = reinterpret_cast<float *>(smem + a.stages * stage_bytes);  // [16, 128]
   WeightsBarriers &bars = *reinterpret_cast<WeightsBarriers *>(sums + 16 * 128);
   volatile uint32_t *dead = &bars.dead;
@@ -428,32 +509,36 @@ __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant_
     if (warp == kWarpLoad && lane == 0) {
       int it = 0;
       bool ok = true;
-      for (; it < count; ++it) {
-        const int s = it % a.stages, r = first + it;
-        if (!(ok = tma::wait(bar(bars.empty[s]), (it / a.stages & 1) ^ 1, dead))) break;
-        const uint32_t dst = tc::smem_addr(smem) + s * stage_bytes, f = bar(bars.full[s]);
-        tma::expect(f, (uint32_t)(dz_boxes * (kParts ? 2 : 1) + boxes) * kBoxBytes);
+      Ring at;
+      const uint32_t dst0 = tc::smem_addr(smem), full0 = bar(bars.full[0]), empty0 = bar(bars.empty[0]);
+      for (; it < count; ++it, at.next(a.stages)) {
+        const int r = first + it;
+        if (!(ok = tma::wait(empty0 + at.s * 8, at.parity ^ 1u, dead))) break;
+        const uint32_t dst = dst0 + at.s * stage_bytes, f = full0 + at.s * 8;
+        tma::expect(f, (uint32_t)(dz_boxes * (kParts ? 2 : 1) + boxes) * kWBoxBytes);
         for (int j = 0; j < dz_boxes; ++j) {
-          tma::load(dst + j * kBoxBytes, &a.dy, n0 + j * 64, r * kStep, f);
-          if (kParts) tma::load(dst + (2 + j) * kBoxBytes, &a.z, n0 + j * 64, r * kStep, f);
+          tma::load(dst + j * kWBoxBytes, &a.dy, n0 + j * 64, r * kWStep, f);
+          if (kParts) tma::load(dst + (2 + j) * kWBoxBytes, &a.z, n0 + j * 64, r * kWStep, f);
         }
-        for (int j = 0; j < boxes; ++j) tma::load(dst + kStageA + j * kBoxBytes, &a.x, k0 + j * 64, r * kStep, f);
+        for (int j = 0; j < boxes; ++j) tma::load(dst + kStageA + j * kWBoxBytes, &a.x, k0 + j * 64, r * kWStep, f);
       }
       if (!ok)
         for (int k = it > a.stages ? it - a.stages : 0; k < it; ++k)
-          for (int t = 0; t < (1 << 16) && !tma::try_wait(bar(bars.full[k % a.stages]), k / a.stages & 1); ++t) {}
+          tma::settle(bar(bars.full[k % a.stages]), k / a.stages & 1);
     } else if (warp == kWarpMma && lane == 0) {
       const uint32_t desc = idesc_of<T>((cols + 15) & ~15, true, true);
-      for (int it = 0; it < count; ++it) {
-        const int s = it % a.stages, group = it / kFlush;
+      const uint64_t a_desc = desc_swizzled(tc::smem_addr(smem), kWBoxBytes), b_desc = a_desc + (kStageA >> 4), stage16 = stage_bytes >> 4;
+      const uint32_t ready0 = touched ? bar(bars.ready[0]) : bar(bars.full[0]), empty0 = bar(bars.empty[0]);
+      Ring at;
+      for (int it = 0; it < count; ++it, at.next(a.stages)) {
+        const int group = it / kFlush;
         // accumulator of this group: one of two in turn, or the first one always
         const int buf = kLow ? 0 : group & 1, use = kLow ? group : group >> 1;
-        if (!tma::wait(touched ? bar(bars.ready[s]) : bar(bars.full[s]), it / a.stages & 1, dead)) break;
-        const uint32_t A = tc::smem_addr(smem) + s * stage_bytes, B = A + kStageA;
+        const uint64_t da = a_desc + at.s * stage16, db = b_desc + at.s * stage16;
+        if (!tma::wait(ready0 + at.s * 8, at.parity, dead)) break;
         auto part = [&](int p, uint32_t d, bool add) {
 #pragma unroll
-          for (int ks = 0; ks < 4; ++ks)
-            tc::mma(d, desc_swizzled(A + p * 2 * kBoxBytes + ks * 2048, kBoxBytes), desc_swizzled(B + ks * 2048, kBoxBytes), add || ks ? 1u : 0u, desc);
+          for (int ks = 0; ks < kWStep / 16; ++ks) tc::mma(d, da + p * (2 * kWBoxBytes >> 4) + ks * 128, db + ks * 128, add || ks ? 1u : 0u, desc);
         };
         tc::fence_after_sync();
         if (kLow) part(1, tmem + second, it > 0);
@@ -461,12 +546,12 @@ __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant_
         if (it % kFlush == 0 && !tma::wait(bar(bars.sum_empty[buf]), (use & 1) ^ 1, dead)) break;
         tc::fence_after_sync();
         part(0, tmem + buf * second, it % kFlush > 0);
-        tc::commit(bar(bars.empty[s]));
+        tc::commit(empty0 + at.s * 8);
         if (it % kFlush == kFlush - 1 || it == count - 1) tc::commit(bar(bars.sum_full[buf]));
       }
       // products in flight end before tensor memory is given back
       tc::commit(bar(bars.done));
-      for (int t = 0; t < (1 << 20) && !tma::try_wait(bar(bars.done), 0u); ++t) {}
+      tma::settle(bar(bars.done), 0u);
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
@@ -475,9 +560,10 @@ __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant_
     const int t = threadIdx.x - kWarpWorker * 32, half = t >> 7, n = n0 + (t & 127);
     const uint32_t lanes = tmem + ((uint32_t)(t & 96) << 16) + half * 128;
     const int chunk = (t & 7) | (t >> 4 & 8), row0 = (t >> 3) & 15;
-    float mine[8], acc[128];
+    float2 mine[4];
+    float acc[128];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) mine[i] = 0.f;
+    for (int i = 0; i < 4; ++i) mine[i] = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < 128; ++i) acc[i] = 0.f;
     bool ok = true;
@@ -499,23 +585,28 @@ __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant_
       if (lane == 0) tma::arrive(bar(bars.sum_empty[buf]));
     };
     // an accumulator is emptied a step after its last one was made ready: the products have time
-    for (int it = 0; ok && it < count; ++it) {
+    Ring at;
+    for (int it = 0; ok && it < count; ++it, at.next(a.stages)) {
       if (touched) {
-        const int s = it % a.stages;
-        if (!(ok = __all_sync(0xffffffffu, tma::wait(bar(bars.full[s]), it / a.stages & 1, dead)))) break;
-        unsigned char *A = smem + s * stage_bytes + (chunk >> 3) * kBoxBytes;
+        const int s = at.s;
+        if (!(ok = __all_sync(0xffffffffu, tma::wait(bar(bars.full[s]), at.parity, dead)))) break;
+        unsigned char *A = smem + s * stage_bytes + (chunk >> 3) * kWBoxBytes;
+        // (rows 16 apart have the same swizzle)
+        auto in = [&](int u) { return A + (row0 + 16 * u) * (int)tma::kRowBytes + (((chunk & 7) ^ (row0 & 7)) * 16); };
         if ((chunk >> 3) < dz_boxes) {
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int row = row0 + 16 * u;
-            const uint32_t at = (uint32_t)row * tma::kRowBytes + (uint32_t)((chunk & 7) ^ (row & 7)) * 16u;
+          for (int u = 0; u < kWStep / 16; u += 2) {
+            const uint4 dy0 = shared16(in(u)), dy1 = shared16(in(u + 1));
             if constexpr (kParts > 0) {
-              transform_chunk<T, kParts, kScale, true>(A + at, A + 2 * kBoxBytes + at, A + 4 * kBoxBytes + at, a.act, mine);
+              const uint4 z0 = shared16(in(u) + 2 * kWBoxBytes), z1 = shared16(in(u + 1) + 2 * kWBoxBytes);
+              transform_chunk<T, kAct, kParts, kScale, true>(in(u), in(u) + 2 * kWBoxBytes, in(u) + 4 * kWBoxBytes, dy0, z0, mine);
+              transform_chunk<T, kAct, kParts, kScale, true>(in(u + 1), in(u + 1) + 2 * kWBoxBytes, in(u + 1) + 4 * kWBoxBytes, dy1, z1, mine);
             } else {
-              float v[8];
-              unpack<T>(*reinterpret_cast<const uint4 *>(A + at), v);
+              float2 v[4], w[4];
+              unpack<T>(dy0, &v[0].x);
+              unpack<T>(dy1, &w[0].x);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) mine[i] += v[i];
+              for (int i = 0; i < 4; ++i) mine[i] = add2(mine[i], add2(v[i], w[i]));
             }
           }
         }
@@ -560,7 +651,7 @@ __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant_
     }
     if (db) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sums[row0 * 128 + chunk * 8 + i] = mine[i];
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<float2 *>(sums + row0 * 128 + chunk * 8 + 2 * i) = mine[i];
       named_sync(2, kWorkerWarps * 32);
       if (t < 128 && n < a.n) {
         float v = 0.f;
@@ -604,36 +695,39 @@ uint32_t tmem_columns(uint32_t n) {
   return c;
 }
 
-// The shape of a call of k_dense_rows: tile width, weights resident or not, pipeline depth.
+// The shape of a call of k_dense_rows: tile width, weights resident or not, pipeline depth.  False where it does not fit.
+bool shape_rows(RowsArgs &a, bool forward, bool transform, int bn, bool resident, int want, uint32_t &smem) {
+  a.bn = bn;
+  a.n_tiles = ceil_div(a.out_cols, bn);
+  a.b_bytes = forward ? (uint32_t)bn * tma::kRowBytes : (uint32_t)ceil_div(bn, 64) * kBoxBytes;
+  a.resident = resident;
+  const uint32_t stage = (transform ? 2 : 1) * kTileBytes + (resident ? 0u : a.b_bytes);
+  const uint64_t fixed = 1024 + 1024 + sizeof(RowsBarriers) + (resident ? (uint64_t)a.k_blocks * a.b_bytes : 0u);
+  for (a.out_slots = 4; a.out_slots >= 2; a.out_slots -= 2) {
+    a.keep_slots = !a.has_keep ? 0 : a.has_residual ? 2 : a.out_slots;
+    const uint64_t used = fixed + (uint64_t)(a.out_slots + a.keep_slots) * kTileBytes;
+    if (used + (uint64_t)want * stage > kSmemMost) continue;
+    a.stages = (int)((kSmemMost - used) / stage);
+    if (a.stages > kMaxStages) a.stages = kMaxStages;
+    smem = (uint32_t)used + (uint32_t)a.stages * stage;
+    return true;
+  }
+  return false;
+}
 bool plan_rows(RowsArgs &a, bool forward, bool transform, int num_sms, uint32_t &smem, int &grid) {
-  const uint32_t stage_a = transform ? 2 * kTileBytes : kTileBytes;
-  const int outputs = 1 + a.has_keep + a.has_residual;
-  auto shape = [&](int bn) {
-    a.bn = bn;
-    a.n_tiles = ceil_div(a.out_cols, bn);
-    a.b_bytes = forward ? (uint32_t)bn * tma::kRowBytes : (uint32_t)ceil_div(bn, 64) * kBoxBytes;
-    const uint32_t fixed = 1024 + 1024 + sizeof(RowsBarriers);
-    for (int resident = 1; resident >= 0; --resident)
-      for (int want = 3; want >= 2; --want)             // rather a deeper pipeline than a second tile on its way out
-      for (int staging = 2; staging >= 1; --staging) {
-        const uint32_t used = fixed + (uint32_t)(outputs * staging) * kTileBytes + (resident ? (uint32_t)a.k_blocks * a.b_bytes : 0u);
-        const uint32_t stage = stage_a + (resident ? 0u : a.b_bytes);
-        if (used + want * stage > kSmemMost) continue;
-        int stages = (int)((kSmemMost - used) / stage);
-        if (stages > kMaxStages) stages = kMaxStages;
-        a.resident = resident; a.staging = staging; a.stages = stages;
-        smem = used + (uint32_t)stages * stage;
-        return true;
-      }
-    return false;
-  };
   // Wide tiles read the rows once; narrower ones where there are fewer tiles than SMs.  Results leave in boxes of 64 columns, so tiles
   // beside one another are a multiple of that.
   int bn = a.out_cols <= 256 ? (a.out_cols + 15) / 16 * 16 : 256;
   while (bn > 64 && (int64_t)a.m_tiles * ceil_div(a.out_cols, bn) * 2 <= num_sms) bn = (bn / 2 + 63) / 64 * 64;
   if (!forward) bn = (bn + 63) / 64 * 64;
-  if (!shape(bn)) return false;
-  a.tmem_cols = tmem_columns(2u * (((uint32_t)bn + 63u) & ~63u));
+  const int narrow = bn > 128 ? 128 : bn;
+  // Resident weights, rather of a narrower tile than not; then a pipeline of three steps; where dz is made, which costs more than
+  // a second look at the rows, wide tiles first.
+  const bool found = (transform && shape_rows(a, forward, transform, bn, true, 2, smem)) || shape_rows(a, forward, transform, bn, true, 3, smem) ||
+                     shape_rows(a, forward, transform, narrow, true, 3, smem) || shape_rows(a, forward, transform, bn, false, 3, smem) ||
+                     shape_rows(a, forward, transform, narrow, false, 2, smem);
+  if (!found) return false;
+  a.tmem_cols = tmem_columns(2u * (((uint32_t)a.bn + 63u) & ~63u));
   int groups = num_sms / a.n_tiles;
   if (groups < 1) groups = 1;
   if (groups > a.m_tiles) groups = a.m_tiles;
@@ -641,10 +735,27 @@ bool plan_rows(RowsArgs &a, bool forward, bool transform, int num_sms, uint32_t 
   return true;
 }
 
-template <class T, bool kForward, int kParts>
-void run_rows(const RowsArgs &a, uint32_t smem, int grid, cudaStream_t st) {
-  cudaFuncSetAttribute(k_dense_rows<T, kForward, kParts>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  launch_chained(k_dense_rows<T, kForward, kParts>, grid, kParts ? 512 : 256, smem, st, a);
+// Once for every kernel and device: all of the SM's shared memory may be asked for.
+template <class Kernel>
+void opt_in(Kernel kernel, std::atomic<uint64_t> &devices) {
+  int device = 0;
+  cudaGetDevice(&device);
+  const uint64_t bit = 1ull << (device & 63);
+  if (device < 64 && (devices.load(std::memory_order_relaxed) & bit)) return;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost) == cudaSuccess) devices.fetch_or(bit, std::memory_order_relaxed);
+}
+template <class T, bool kForward, int kAct>
+void run_rows_as(const RowsArgs &a, uint32_t smem, int grid, cudaStream_t st) {
+  static std::atomic<uint64_t> devices{0};
+  opt_in(k_dense_rows<T, kForward, kAct>, devices);
+  launch_chained(k_dense_rows<T, kForward, kAct>, grid, kRowsThreads<kForward, kRowsParts<kForward, kAct>>, smem, st, a);
+}
+template <class T, bool kForward>
+void run_rows(int act, const RowsArgs &a, uint32_t smem, int grid, cudaStream_t st) {
+  if (act == GS_DENSE_NONE) run_rows_as<T, kForward, GS_DENSE_NONE>(a, smem, grid, st);
+  else if (act == GS_DENSE_RELU) run_rows_as<T, kForward, GS_DENSE_RELU>(a, smem, grid, st);
+  else if (act == GS_DENSE_SILU) run_rows_as<T, kForward, GS_DENSE_SILU>(a, smem, grid, st);
+  else run_rows_as<T, kForward, GS_DENSE_GELU>(a, smem, grid, st);
 }
 
 template <class T>
@@ -652,7 +763,7 @@ int fwd(const DenseArgs &d, int num_sms, cudaStream_t st) {
   RowsArgs a;
   a.bias = d.bias; a.out_cols = d.out; a.k = d.in; a.k_blocks = ceil_div(d.in, kStep); a.m_tiles = ceil_div(d.rows, kRows);
   a.rows = (int)d.rows; a.out_rows = d.y; a.ld_out = d.ld_y; a.keep_rows = d.preact; a.ld_keep = d.ld_preact;
-  a.act = d.act; a.has_keep = d.preact != nullptr; a.has_residual = d.residual != nullptr; a.timeout = d.timeout;
+  a.has_keep = d.preact != nullptr; a.has_residual = d.residual != nullptr; a.timeout = d.timeout;
   uint32_t smem;
   int grid;
   if (!plan_rows(a, true, false, num_sms, smem, grid)) return -1;
@@ -661,7 +772,7 @@ int fwd(const DenseArgs &d, int num_sms, cudaStream_t st) {
       (d.out >= 8 && a.has_keep && !tma::make_map(&a.keep, d.dtype, d.preact, d.rows, d.out & ~7, d.ld_preact, kRows)) ||
       (a.has_residual && !tma::make_map(&a.residual, d.dtype, d.residual, d.rows, d.out, d.ld_residual, kRows)))
     return -1;
-  run_rows<T, true, 0>(a, smem, grid, st);
+  run_rows<T, true>(d.act, a, smem, grid, st);
   return 1;
 }
 
@@ -682,28 +793,29 @@ WeightsPlan plan_weights(int64_t rows, int in, int out, int num_sms) {
   return p;
 }
 
-template <class T, int kParts, bool kScale>
+template <class T, int kAct>
 void run_weights(WeightsArgs &a, cudaStream_t st) {
-  const uint32_t stage = ((kParts == 3 ? 3u : kParts ? 2u : 1u) * 2u + (uint32_t)ceil_div(a.bk, 64)) * kBoxBytes;
+  constexpr int kParts = weight_parts<T>(kAct);
+  const uint32_t stage = ((kParts == 3 ? 3u : kParts ? 2u : 1u) * 2u + (uint32_t)ceil_div(a.bk, 64)) * kWBoxBytes;
   const uint32_t fixed = 1024 + 16 * 128 * 4 + sizeof(WeightsBarriers);
   a.stages = (int)((kSmemMost - fixed) / stage);
   if (a.stages > kMaxStages) a.stages = kMaxStages;
   const uint32_t smem = fixed + a.stages * stage;
   a.tmem_cols = a.bk > 128 ? 512u : 256u;
-  cudaFuncSetAttribute(k_dense_weights<T, kParts, kScale>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  launch_chained(k_dense_weights<T, kParts, kScale>, a.n_tiles * a.k_tiles * a.splits, 384, smem, st, a);
+  static std::atomic<uint64_t> devices{0};
+  opt_in(k_dense_weights<T, kAct>, devices);
+  launch_chained(k_dense_weights<T, kAct>, a.n_tiles * a.k_tiles * a.splits, 384, smem, st, a);
 }
 
 template <class T>
 int bwd(const DenseArgs &d, int num_sms, cudaStream_t st) {
-  constexpr bool kHalf = __is_same(T, __half);
-  const bool plain = d.act == GS_DENSE_NONE, relu = d.act == GS_DENSE_RELU;
+  const bool plain = d.act == GS_DENSE_NONE;
   int launches = 0;
   if (d.dx) {
     RowsArgs a;
     a.bias = nullptr; a.out_cols = d.in; a.k = d.out; a.k_blocks = ceil_div(d.out, kStep); a.m_tiles = ceil_div(d.rows, kRows);
     a.rows = (int)d.rows; a.out_rows = d.dx; a.ld_out = d.ld_dx; a.keep_rows = nullptr; a.ld_keep = 0;
-    a.act = d.act; a.has_keep = a.has_residual = 0; a.timeout = d.timeout;
+    a.has_keep = a.has_residual = 0; a.timeout = d.timeout;
     uint32_t smem;
     int grid;
     if (!plan_rows(a, false, !plain, num_sms, smem, grid)) return -1;
@@ -711,25 +823,23 @@ int bwd(const DenseArgs &d, int num_sms, cudaStream_t st) {
         (d.in >= 8 && !tma::make_map(&a.out, d.dtype, d.dx, d.rows, d.in & ~7, d.ld_dx, kRows)) ||
         (!plain && !tma::make_map(&a.z, d.dtype, d.preact_in, d.rows, d.out, d.ld_preact, kRows)))
       return -1;
-    if (plain) run_rows<T, false, 0>(a, smem, grid, st);
-    else if (relu) run_rows<T, false, 1>(a, smem, grid, st);
-    else run_rows<T, false, 2>(a, smem, grid, st);
+    run_rows<T, false>(d.act, a, smem, grid, st);
     ++launches;
   }
   if (d.dw) {
     const WeightsPlan p = plan_weights(d.rows, d.in, d.out, num_sms < kSplitSms ? num_sms : kSplitSms);
     WeightsArgs a;
     a.n = d.out; a.k = d.in; a.n_tiles = p.n_tiles; a.k_tiles = p.k_tiles; a.splits = p.splits; a.bk = p.bk; a.ld = p.ld;
-    a.row_blocks = ceil_div(d.rows, kStep); a.act = d.act; a.want_db = d.db != nullptr; a.timeout = d.timeout;
+    a.row_blocks = ceil_div(d.rows, kWStep); a.want_db = d.db != nullptr; a.timeout = d.timeout;
     a.partials = d.partials;
     a.db_partials = d.partials + (size_t)p.splits * d.out * p.ld;
-    if (!tma::make_map(&a.dy, d.dtype, d.dy, d.rows, d.out, d.ld_dy, kStep) || !tma::make_map(&a.x, d.dtype, d.x, d.rows, d.in, d.ld_x, kStep) ||
-        (!plain && !tma::make_map(&a.z, d.dtype, d.preact_in, d.rows, d.out, d.ld_preact, kStep)))
+    if (!tma::make_map(&a.dy, d.dtype, d.dy, d.rows, d.out, d.ld_dy, kWStep) || !tma::make_map(&a.x, d.dtype, d.x, d.rows, d.in, d.ld_x, kWStep) ||
+        (!plain && !tma::make_map(&a.z, d.dtype, d.preact_in, d.rows, d.out, d.ld_preact, kWStep)))
       return -1;
-    if (plain) run_weights<T, 0, false>(a, st);
-    else if (relu) run_weights<T, 1, false>(a, st);
-    else if constexpr (kHalf) run_weights<T, 2, true>(a, st);
-    else run_weights<T, 3, false>(a, st);
+    if (d.act == GS_DENSE_NONE) run_weights<T, GS_DENSE_NONE>(a, st);
+    else if (d.act == GS_DENSE_RELU) run_weights<T, GS_DENSE_RELU>(a, st);
+    else if (d.act == GS_DENSE_SILU) run_weights<T, GS_DENSE_SILU>(a, st);
+    else run_weights<T, GS_DENSE_GELU>(a, st);
     launch_chained(k_dense_sums, ceil_div((int64_t)d.out * p.ld + (d.db ? d.out : 0), 256), 256, 0, st, (const float *)a.partials,
                    (const float *)a.db_partials, p.splits, d.out, d.in, p.ld, d.dw, d.db);
     launches += 2;

@@ -6,7 +6,8 @@
 // A pure stream: forward reads x and writes y once, backward reads x and dy and writes dx once, so HBM bounds it.  A row
 // lives in the registers of a group of lanes (1 to 32 of a warp, or the 256 of a CTA), as the vectors of 16 bytes it was
 // loaded in; the variance is taken about the mean in a second pass over the registers, which loses nothing where the mean is
-// large against the spread.  All sums in fp32.  The grid is persistent: a lane keeps its columns from row to row, so
+// large against the spread.  All sums in fp32, two operations an instruction (add2 and the like): with one each the arithmetic
+// was the bound (1M rows of 256 took 349 us forward, 432 backward; together with the row fetched ahead 189 and 282).  The grid is persistent: a lane keeps its columns from row to row, so
 // gamma and beta stay in registers, and in the backward so do its sums for dgamma and dbeta, which leave as one row of partial
 // sums per CTA and are added up by k_layer_norm_sums in a fixed order (no atomics: the same bits from run to run).
 #include <cuda_bf16.h>
@@ -22,8 +23,14 @@ namespace {
 constexpr int kNormThreads = 256;
 constexpr int kNormPartialRows = 592;     // most CTAs of the backward
 
+// CTAs per SM, of as many registers as the elements of a lane need, and no more CTAs than are resident: 1M rows of 256 in bf16
+// forward 189 us with three, 221 with four (spills), 308 with two; backward in fp16 282 with two, 324 with the compiler's choice.
+__host__ __device__ constexpr int fwd_ctas(int elements) { return elements <= 8 ? 6 : elements <= 16 ? 3 : 1; }
+__host__ __device__ constexpr int bwd_ctas(int elements) { return elements <= 8 ? 3 : elements <= 16 ? 2 : 1; }
+
 // How a row is laid over lanes: `lanes` of them with NV vectors of V elements each, vector j of lane l at column (j lanes + l) V.
-template <class T, int V, int NV, bool kBlock>
+// V is a whole 16-byte vector, or 1 where rows are not aligned.
+template <class T, int V, int NV>
 struct Row {
   uint4 raw[V > 1 ? NV : 1];
   float one[V > 1 ? 1 : NV];
@@ -46,48 +53,61 @@ struct Row {
       }
     }
   }
-  __device__ __forceinline__ void get(int j, float v[V]) const {
-    if constexpr (V > 1) unpack<T>(raw[j], v);
-    else v[0] = one[j];
+  __device__ __forceinline__ void get(float2 v[V * NV / 2]) const {
+    if constexpr (V > 1) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) unpack<T>(raw[j], &v[j * V / 2].x);
+    } else {
+#pragma unroll
+      for (int j = 0; j < NV / 2; ++j) v[j] = make_float2(one[2 * j], one[2 * j + 1]);
+    }
   }
 };
-template <class T, int V>
-__device__ __forceinline__ void put(T *p, int c, int cols, const float v[V]) {
-  if constexpr (V > 1) {
-    if (c + V <= cols) { __stcs(reinterpret_cast<uint4 *>(p + c), pack<T>(v)); return; }
-  }
+// A lane's values to where they belong.
+template <class T, int V, int NV>
+__device__ __forceinline__ void put(T *p, int lane, int lanes, int cols, const float2 v2[V * NV / 2]) {
+  const float *v = &v2[0].x;
 #pragma unroll
-  for (int i = 0; i < V; ++i)
-    if (c + i < cols) p[c + i] = narrow<T>(v[i]);
+  for (int j = 0; j < NV; ++j) {
+    const int c = (j * lanes + lane) * V;
+    if constexpr (V > 1) {
+      if (c + V <= cols) { __stcs(reinterpret_cast<uint4 *>(p + c), pack<T>(v + j * V)); continue; }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (c + i < cols) p[c + i] = narrow<T>(v[j * V + i]);
+  }
 }
 
-// Sum over a group; in the order of the lanes' numbers, the same in every lane.
+// Sums over a group; the same in every lane.
 template <bool kBlock>
-__device__ __forceinline__ float group_sum(float v, int lanes, float *shared) {
-  if constexpr (!kBlock) {
-    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-  } else {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+__device__ __forceinline__ float2 group_sum2(float2 v, int lanes, float2 *shared) {
+  for (int o = (kBlock ? 32 : lanes) >> 1; o > 0; o >>= 1)
+    v = add2(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+  if constexpr (kBlock) {
     __syncthreads();
     if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
     __syncthreads();
     v = shared[0];
 #pragma unroll
-    for (int w = 1; w < kNormThreads / 32; ++w) v += shared[w];
-    return v;
+    for (int w = 1; w < kNormThreads / 32; ++w) v = add2(v, shared[w]);
   }
+  return v;
 }
 template <bool kBlock>
-__device__ __forceinline__ float2 group_sum2(float2 v, int lanes, float *shared) {
-  const float a = group_sum<kBlock>(v.x, lanes, shared);
-  return make_float2(a, group_sum<kBlock>(v.y, lanes, shared));
+__device__ __forceinline__ float group_sum(float v, int lanes, float2 *shared) {
+  if constexpr (kBlock) {
+    return group_sum2<true>(make_float2(v, 0.f), lanes, shared).x;
+  } else {
+    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  }
 }
 
 // A lane's values of a parameter vector.
 template <int V, int NV>
-__device__ __forceinline__ void columns(const float *p, float fallback, int lane, int lanes, int cols, float out[V * NV]) {
+__device__ __forceinline__ void columns(const float *p, float fallback, int lane, int lanes, int cols, float2 out2[V * NV / 2]) {
+  float *out = &out2[0].x;
 #pragma unroll
   for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -97,54 +117,47 @@ __device__ __forceinline__ void columns(const float *p, float fallback, int lane
     }
 }
 
+// The next row is asked for before this one's sums are taken, where a row is short enough for the registers.
 template <class T, int V, int NV, bool kBlock>
-__global__ void __launch_bounds__(kNormThreads) k_layer_norm_fwd(LayerNormArgs a, int lanes) {
-  __shared__ float shared[kNormThreads / 32];
+__global__ void __launch_bounds__(kNormThreads, fwd_ctas(V * NV)) k_layer_norm_fwd(LayerNormArgs a, int lanes) {
+  __shared__ float2 shared[kNormThreads / 32];
+  constexpr int P = V * NV / 2;
   dependency_wait();
   const int group = kBlock ? 0 : threadIdx.x / lanes, lane = kBlock ? threadIdx.x : threadIdx.x & (lanes - 1);
   const int groups = kBlock ? 1 : kNormThreads / lanes;
-  float gamma[V * NV], beta[V * NV];
+  float2 gamma[P], beta[P];
   columns<V, NV>(a.gamma, 1.f, lane, lanes, a.cols, gamma);
   columns<V, NV>(a.beta, 0.f, lane, lanes, a.cols, beta);
   const float inv = 1.f / (float)a.cols;
-  for (int64_t row0 = (int64_t)blockIdx.x * groups; row0 < a.rows; row0 += (int64_t)gridDim.x * groups) {
-    const int64_t row = row0 + group;
-    const bool live = row < a.rows;
-    Row<T, V, NV, kBlock> x;
-    x.load(static_cast<const T *>(a.x) + row * a.ld_x, lane, lanes, a.cols, live);
-    float s = 0.f;
+  const bool ragged = lanes * NV * V != a.cols;
+  const int64_t step = (int64_t)gridDim.x * groups;
+  int64_t row = (int64_t)blockIdx.x * groups + group;
+  Row<T, V, NV> x;
+  x.load(static_cast<const T *>(a.x) + row * a.ld_x, lane, lanes, a.cols, row < a.rows);
+  for (int64_t row0 = (int64_t)blockIdx.x * groups; row0 < a.rows; row0 += step, row += step) {
+    float2 v[P];
+    x.get(v);
+    x.load(static_cast<const T *>(a.x) + (row + step) * a.ld_x, lane, lanes, a.cols, row + step < a.rows);
+    float2 s = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      float v[V];
-      x.get(j, v);
+    for (int i = 0; i < P; ++i) s = add2(s, v[i]);
+    const float mean = group_sum<kBlock>(s.x + s.y, lanes, shared) * inv;
+    s = make_float2(0.f, 0.f);
+    const float2 minus = both(-mean);
 #pragma unroll
-      for (int i = 0; i < V; ++i) s += v[i];
+    for (int i = 0; i < P; ++i) v[i] = add2(v[i], minus);
+    if (ragged) {
+#pragma unroll
+      for (int e = 0; e < 2 * P; ++e)
+        if (((e / V) * lanes + lane) * V + e % V >= a.cols) (&v[0].x)[e] = 0.f;
     }
-    const float mean = group_sum<kBlock>(s, lanes, shared) * inv;
-    s = 0.f;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      float v[V];
-      x.get(j, v);
+    for (int i = 0; i < P; ++i) s = fma2(v[i], v[i], s);
+    const float rstd = 1.f / sqrtf(fmaf(group_sum<kBlock>(s.x + s.y, lanes, shared), inv, a.eps));
+    if (row < a.rows) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float d = (j * lanes + lane) * V + i < a.cols ? v[i] - mean : 0.f;
-        s = fmaf(d, d, s);
-      }
-    }
-    const float rstd = 1.f / sqrtf(fmaf(group_sum<kBlock>(s, lanes, shared), inv, a.eps));
-    if (live) {
-      T *y = static_cast<T *>(a.y) + row * a.ld_out;
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int c = (j * lanes + lane) * V;
-        if (c >= a.cols) break;
-        float v[V];
-        x.get(j, v);
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = fmaf((v[i] - mean) * rstd, gamma[j * V + i], beta[j * V + i]);
-        put<T, V>(y, c, a.cols, v);
-      }
+      for (int i = 0; i < P; ++i) v[i] = fma2(mul2(v[i], both(rstd)), gamma[i], beta[i]);
+      put<T, V, NV>(static_cast<T *>(a.y) + row * a.ld_out, lane, lanes, a.cols, v);
       if (lane == 0) {
         if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;
@@ -154,75 +167,73 @@ __global__ void __launch_bounds__(kNormThreads) k_layer_norm_fwd(LayerNormArgs a
 }
 
 template <class T, int V, int NV, bool kBlock, bool kParams>
-__global__ void __launch_bounds__(kNormThreads) k_layer_norm_bwd(LayerNormArgs a, int lanes) {
-  __shared__ float shared[kNormThreads / 32];
-  constexpr int E = V * NV;
+__global__ void __launch_bounds__(kNormThreads, bwd_ctas(V * NV)) k_layer_norm_bwd(LayerNormArgs a, int lanes) {
+  __shared__ float2 shared[kNormThreads / 32];
+  constexpr int P = V * NV / 2;
   dependency_wait();
   const int group = kBlock ? 0 : threadIdx.x / lanes, lane = kBlock ? threadIdx.x : threadIdx.x & (lanes - 1);
   const int groups = kBlock ? 1 : kNormThreads / lanes;
-  float gamma[E], sum_g[E], sum_b[E];
+  float2 gamma[P], sum_g[P], sum_b[P];
   columns<V, NV>(a.gamma, 1.f, lane, lanes, a.cols, gamma);
 #pragma unroll
-  for (int i = 0; i < E; ++i) sum_g[i] = sum_b[i] = 0.f;
+  for (int i = 0; i < P; ++i) sum_g[i] = sum_b[i] = make_float2(0.f, 0.f);
   const float inv = 1.f / (float)a.cols;
-  for (int64_t row0 = (int64_t)blockIdx.x * groups; row0 < a.rows; row0 += (int64_t)gridDim.x * groups) {
-    const int64_t row = row0 + group;
-    const bool live = row < a.rows;
-    Row<T, V, NV, kBlock> x, dy;
-    x.load(static_cast<const T *>(a.x) + row * a.ld_x, lane, lanes, a.cols, live);
-    dy.load(static_cast<const T *>(a.dy) + row * a.ld_dy, lane, lanes, a.cols, live);
-    const float mean = live ? __ldg(a.mean + row) : 0.f, rstd = live ? __ldg(a.rstd + row) : 0.f;
-    float h[E], g[E];
-    float2 s = make_float2(0.f, 0.f);
+  const int64_t step = (int64_t)gridDim.x * groups;
+  int64_t row = (int64_t)blockIdx.x * groups + group;
+  Row<T, V, NV> x, dy;
+  float mean, rstd;
+  auto fetch = [&](int64_t r) {
+    const bool live = r < a.rows;
+    x.load(static_cast<const T *>(a.x) + r * a.ld_x, lane, lanes, a.cols, live);
+    dy.load(static_cast<const T *>(a.dy) + r * a.ld_dy, lane, lanes, a.cols, live);
+    mean = live ? __ldg(a.mean + r) : 0.f;
+    rstd = live ? __ldg(a.rstd + r) : 0.f;
+  };
+  fetch(row);
+  for (int64_t row0 = (int64_t)blockIdx.x * groups; row0 < a.rows; row0 += step, row += step) {
+    float2 h[P], g[P];
+    x.get(h);
+    dy.get(g);
+    const float2 minus = both(-mean), r = both(rstd);
+    fetch(row + step);
+    float2 s = make_float2(0.f, 0.f), t = s;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      float v[V], d[V];
-      x.get(j, v);
-      dy.get(j, d);
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int e = j * V + i;
-        // columns behind the row's end have dy = 0: nothing comes of them whatever h is there
-        h[e] = (v[i] - mean) * rstd;
-        g[e] = d[i] * gamma[e];
-        s.x += g[e];
-        s.y = fmaf(g[e], h[e], s.y);
-        if (kParams) {
-          sum_g[e] = fmaf(d[i], h[e], sum_g[e]);
-          sum_b[e] += d[i];
-        }
+    for (int i = 0; i < P; ++i) {
+      // columns behind the row's end have dy = 0: nothing comes of them whatever h is there
+      h[i] = mul2(add2(h[i], minus), r);
+      if (kParams) {
+        sum_g[i] = fma2(g[i], h[i], sum_g[i]);
+        sum_b[i] = add2(sum_b[i], g[i]);
       }
+      g[i] = mul2(g[i], gamma[i]);
+      s = add2(s, g[i]);
+      t = fma2(g[i], h[i], t);
     }
-    s = group_sum2<kBlock>(s, lanes, shared);
-    if (live && a.dx) {
-      const float avg_g = s.x * inv, avg_gh = s.y * inv;
-      T *dx = static_cast<T *>(a.dx) + row * a.ld_out;
+    const float2 sums = group_sum2<kBlock>(make_float2(s.x + s.y, t.x + t.y), lanes, shared);
+    if (row < a.rows && a.dx) {
+      const float2 avg_g = both(-sums.x * inv), avg_gh = both(-sums.y * inv);
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int c = (j * lanes + lane) * V;
-        if (c >= a.cols) break;
-        float v[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = rstd * (fmaf(-h[j * V + i], avg_gh, g[j * V + i]) - avg_g);
-        put<T, V>(dx, c, a.cols, v);
-      }
+      for (int i = 0; i < P; ++i) g[i] = mul2(add2(fma2(h[i], avg_gh, g[i]), avg_g), r);
+      put<T, V, NV>(static_cast<T *>(a.dx) + row * a.ld_out, lane, lanes, a.cols, g);
     }
   }
   if constexpr (kParams) {
     // one row [2, cols] per CTA: the groups' sums of a column added in their order
+    constexpr int E = 2 * P;
+    const float *gs = &sum_g[0].x, *bs = &sum_b[0].x;
     float *out = a.partials + (size_t)blockIdx.x * 2 * a.cols;
     if constexpr (kBlock) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const int c = ((e / V) * lanes + lane) * V + e % V;
-        if (c < a.cols) { out[c] = sum_g[e]; out[a.cols + c] = sum_b[e]; }
+        if (c < a.cols) { out[c] = gs[e]; out[a.cols + c] = bs[e]; }
       }
     } else {
       __shared__ float part[kNormThreads];
       // (sums of a warp's groups by shuffles, then of the warps through shared memory)
 #pragma unroll
       for (int e = 0; e < 2 * E; ++e) {
-        float v = e < E ? sum_g[e < E ? e : 0] : sum_b[e < E ? 0 : e - E];
+        float v = e < E ? gs[e < E ? e : 0] : bs[e < E ? 0 : e - E];
         for (int o = lanes; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         __syncthreads();
         part[threadIdx.x] = v;
@@ -267,7 +278,7 @@ int lanes_for(int vectors, int nv) {
 template <class T, int V, int NV, bool kBlock>
 int fwd(const LayerNormArgs &a, int lanes, int num_sms, cudaStream_t st) {
   const int64_t groups = kBlock ? 1 : kNormThreads / lanes, want = (a.rows + groups - 1) / groups;
-  const int64_t most = (int64_t)num_sms * 6;
+  const int64_t most = (int64_t)num_sms * fwd_ctas(V * NV);
   launch_chained(k_layer_norm_fwd<T, V, NV, kBlock>, (unsigned)(want < most ? want : most), kNormThreads, 0, st, a, lanes);
   return 1;
 }
@@ -278,7 +289,7 @@ int bwd_grid(int64_t rows, int groups) {
 template <class T, int V, int NV, bool kBlock>
 int bwd(const LayerNormArgs &a, int lanes, int num_sms, cudaStream_t st) {
   int grid = bwd_grid(a.rows, kBlock ? 1 : kNormThreads / lanes);
-  const int most = num_sms * 3;
+  const int most = num_sms * bwd_ctas(V * NV);
   if (grid > most) grid = most;
   if (!a.dgamma && !a.dbeta) {
     launch_chained(k_layer_norm_bwd<T, V, NV, kBlock, false>, grid, kNormThreads, 0, st, a, lanes);
@@ -299,12 +310,13 @@ int fwd_any(const LayerNormArgs &a, int num_sms, cudaStream_t st) {
   const bool vec = vectors_fit(a.x, a.ld_x, a.rows, sizeof(T)) && vectors_fit(a.y, a.ld_out, a.rows, sizeof(T));
   const int n = vec ? (a.cols + V - 1) / V : a.cols;
   if (vec) {
-    constexpr int most = 32 / V;                  // vectors of a lane that holds 32 elements
+    constexpr int few = 16 / V, most = 32 / V;    // vectors of a lane that holds 16 or 32 elements
     if (n <= 4) return fwd<T, V, 1, false>(a, lanes_for(n, 1), num_sms, st);
-    if (n <= 32 * 4) return fwd<T, V, 4, false>(a, lanes_for(n, 4), num_sms, st);
+    if (n <= 32 * few) return fwd<T, V, few, false>(a, lanes_for(n, few), num_sms, st);
+    if (n <= kNormThreads) return fwd<T, V, 1, true>(a, kNormThreads, num_sms, st);
     return fwd<T, V, most, true>(a, kNormThreads, num_sms, st);
   }
-  if (n <= 4) return fwd<T, 1, 1, false>(a, lanes_for(n, 1), num_sms, st);
+  if (n <= 4) return fwd<T, 1, 2, false>(a, lanes_for(n, 2), num_sms, st);
   if (n <= 128) return fwd<T, 1, 4, false>(a, lanes_for(n, 4), num_sms, st);
   if (n <= 2048) return fwd<T, 1, 8, true>(a, kNormThreads, num_sms, st);
   return fwd<T, 1, 32, true>(a, kNormThreads, num_sms, st);
@@ -322,7 +334,7 @@ int bwd_any(const LayerNormArgs &a, int num_sms, cudaStream_t st) {
     if (n <= kNormThreads) return bwd<T, V, 1, true>(a, kNormThreads, num_sms, st);
     return bwd<T, V, most, true>(a, kNormThreads, num_sms, st);
   }
-  if (n <= 4) return bwd<T, 1, 1, false>(a, lanes_for(n, 1), num_sms, st);
+  if (n <= 4) return bwd<T, 1, 2, false>(a, lanes_for(n, 2), num_sms, st);
   if (n <= 128) return bwd<T, 1, 4, false>(a, lanes_for(n, 4), num_sms, st);
   if (n <= 2048) return bwd<T, 1, 8, true>(a, kNormThreads, num_sms, st);
   return bwd<T, 1, 32, true>(a, kNormThreads, num_sms, st);

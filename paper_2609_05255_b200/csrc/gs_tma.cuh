@@ -52,19 +52,28 @@ __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.ar
 __device__ __forceinline__ void init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
   uint32_t done;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(done) : "r"(bar), "r"(parity), "r"(1000u) : "memory");
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
   return done != 0;
 }
-// Waits for a phase, at most about two seconds (each try sleeps about a microsecond at most) or until another role of the CTA
-// has given up.  Who gives up says so in *dead: everybody's waits then end, and the CTA leaves in order.
+// Waits for a phase, at most 2^32 cycles (about two seconds) or until another role of the CTA has given up.  Who gives up says so
+// in *dead: everybody's waits then end, and the CTA leaves in order.
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t *dead) {
-  for (int it = 0; it < (1 << 21); ++it) {
-    if (try_wait(bar, parity)) return true;
-    if ((it & 63) == 63 && *dead) return false;
+  if (try_wait(bar, parity)) return true;
+  const long long begin = clock64();
+  while (!try_wait(bar, parity)) {
+    if (*dead) return false;
+    if (clock64() - begin > (1ll << 32)) {
+      *dead = 1u;
+      return false;
+    }
   }
-  *dead = 1u;
-  return false;
+  return true;
+}
+// The same without a word to the others: for what has to end before a CTA leaves.
+__device__ __forceinline__ void settle(uint32_t bar, uint32_t parity) {
+  const long long begin = clock64();
+  while (!try_wait(bar, parity) && clock64() - begin < (1ll << 28)) {}
 }
 #endif
 
