@@ -513,10 +513,10 @@ class AdamTensor:
         self._more = (_vp * max(1, len(self.more_grads)))(*[_ptr(g) for g in self.more_grads])
 
     def c_struct(self) -> GsAdamTensor:
-        more = C.cast(self._more, C.POINTER(_vp)) if self.more_grads else None
+        # (arrays become pointers where they are assigned to pointer fields, and stay referenced by the struct)
         return GsAdamTensor(_ptr(self.param), _ptr(self.grad), _ptr(self.exp_avg), _ptr(self.exp_avg_sq), _ptr(self.half_copy),
-                            self.rows, self.cols, C.cast(self.lr, C.POINTER(C.c_float)), self.beta1, self.beta2, self.eps,
-                            more, len(self.more_grads))
+                            self.rows, self.cols, self.lr, self.beta1, self.beta2, self.eps,
+                            self._more if self.more_grads else None, len(self.more_grads))
 
 
 def gs_adam_step(ctx: Context, tensors, step: int, stream=None) -> None:

@@ -59,7 +59,8 @@ __global__ void __launch_bounds__(kAdamThreads) k_adam(const __grid_constant__ A
     scale = __ldg(clip + 1);
   }
   const uint32_t total_chunks = a.chunk_start[a.num_tensors];
-  for (uint32_t chunk = blockIdx.x; chunk < total_chunks; chunk += gridDim.x) {
+  for (uint32_t at = blockIdx.x; at < total_chunks; at += gridDim.x) {
+    const uint32_t chunk = kClip ? total_chunks - 1 - at : at;    // (what the norm has read last is in the L2)
     int ti = 0;
     while (ti + 1 < a.num_tensors && chunk >= a.chunk_start[ti + 1]) ++ti;
     const AdamTensorDev &t = a.t[ti];

@@ -43,7 +43,7 @@ struct GradArgs {
   GradEntry t[kTensors];
   const void *more[kMore];
 };
-using GradArgsSmall = GradArgs<24, 64>;
+using GradArgsSmall = GradArgs<64, 128>;
 using GradArgsLarge = GradArgs<GS_GRAD_MAX_TENSORS, GS_GRAD_MAX_BUFFERS>;
 static_assert(sizeof(GradArgsLarge) <= 32000, "kernel parameters end at 32764 bytes");
 
@@ -57,54 +57,86 @@ __device__ __forceinline__ int entry_of(const Args &a, uint32_t chunk) {
   return lo;
 }
 
-// Calls vec(values, element) for whole vectors and one(value, element) for single elements of the sums s of a chunk.
-template <class T, class Args, class Vec, class One>
+// Calls vec(values, element) for whole vectors and one(value, element) for single elements of the sums s of a chunk.  Several vectors
+// are asked for before the first is used: four, or with further buffers (kMore) those of four buffers at one or two places (one
+// buffer after another is waited for one after another: the norm of eight buffers of 25M elements took about 195 us, 113 so; 122 are
+// the bytes' time).
+template <class T, bool kMore, class Args, class Vec, class One>
 __device__ __forceinline__ void chunk_sums(const Args &a, const GradEntry &t, uint32_t chunk, Vec vec, One one) {
-  constexpr int V = kVecOf<T>;
+  constexpr int V = kVecOf<T>, U = kMore ? 8 / V : 4, B = kMore ? 4 : 1;
   const T *g = static_cast<const T *>(t.grad);
   const uint64_t head = t.head == 0xffffffffu ? t.count : t.head;
   const uint64_t begin = (uint64_t)(chunk - t.chunk_start) * kGradChunk, end = min(begin + kGradChunk, t.count);
-  auto single = [&](uint64_t e) {
-    float s = widen(g[e]);
-    for (int k = 0; k < t.num_more; ++k) s += widen(static_cast<const T *>(a.more[t.more_start + k])[e]);
-    one(s, e);
-  };
   // vectors start at head + i V: those that start inside [begin, end) and are whole belong to the chunk, so do the single elements
   const uint64_t first = begin <= head ? head : head + (begin - head + V - 1) / V * V;
   const uint64_t last = t.count < head + V ? head : head + (t.count - head) / V * V;      // end of the whole vectors
-  constexpr int kUnroll = kGradChunk / (kGradThreads * V);
+  const uint64_t stop = min(end, last);
+  const int vectors = first < stop ? (int)((stop - first + V - 1) / V) : 0;
+  const int buffers = 1 + (kMore ? t.num_more : 0);
+  for (int v0 = threadIdx.x; v0 < vectors; v0 += U * kGradThreads) {
+    const uint64_t e0 = first + (uint64_t)v0 * V;
+    if constexpr (!kMore) {
+      uint4 raw[U];
 #pragma unroll
-  for (int half = 0; half < (kUnroll + 3) / 4; ++half) {
-    uint4 raw[4];
-    uint64_t e[4];
+      for (int u = 0; u < U; ++u)
+        if (v0 + u * kGradThreads < vectors) raw[u] = *reinterpret_cast<const uint4 *>(g + e0 + u * kGradThreads * V);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      e[u] = first + (uint64_t)((half * 4 + u) * kGradThreads + threadIdx.x) * V;
-      if (e[u] < end && e[u] < last) raw[u] = *reinterpret_cast<const uint4 *>(g + e[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (e[u] < end && e[u] < last) {
-        float s[V];
-        unpack<T>(raw[u], s);
-        for (int k = 0; k < t.num_more; ++k) {
-          float x[V];
-          unpack<T>(*reinterpret_cast<const uint4 *>(static_cast<const T *>(a.more[t.more_start + k]) + e[u]), x);
-#pragma unroll
-          for (int i = 0; i < V; ++i) s[i] += x[i];
+      for (int u = 0; u < U; ++u)
+        if (v0 + u * kGradThreads < vectors) {
+          float s[V];
+          unpack<T>(raw[u], s);
+          vec(s, e0 + u * kGradThreads * V);
         }
-        vec(s, e[u]);
+    } else {
+      float s[U][V];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[u][i] = -0.f;           // (adds nothing, also to a zero of either sign)
+#pragma unroll 1
+      for (int k0 = 0; k0 < buffers; k0 += B) {
+        uint4 raw[B][U];
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+          const T *p = (k0 + k > 0 && k0 + k < buffers ? static_cast<const T *>(a.more[t.more_start + k0 + k - 1]) : g) + e0;
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            raw[k][u] = make_uint4(0u, 0u, 0u, 0u);
+            if (k0 + k < buffers && v0 + u * kGradThreads < vectors) raw[k][u] = *reinterpret_cast<const uint4 *>(p + u * kGradThreads * V);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < B; ++k)
+          if (k0 + k < buffers) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              float x[V];
+              unpack<T>(raw[k][u], x);
+#pragma unroll
+              for (int i = 0; i < V; ++i) s[u][i] += x[i];
+            }
+          }
       }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (v0 + u * kGradThreads < vectors) vec(s[u], e0 + u * kGradThreads * V);
+    }
   }
+  auto single = [&](uint64_t e) {
+    float s = widen(g[e]);
+    for (int k = 0; k < buffers - 1; ++k) s += widen(static_cast<const T *>(a.more[t.more_start + k])[e]);
+    one(s, e);
+  };
   for (uint64_t e = begin + threadIdx.x; e < min(end, head); e += kGradThreads) single(e);
   for (uint64_t e = max(begin, max(last, head)) + threadIdx.x; e < end; e += kGradThreads) single(e);
 }
 
-template <int V>
+template <int V, bool kInRange = false>
 __device__ __forceinline__ double squares(const float s[V]) {
-  float most = 0.f;
+  float most = kInRange ? 1.f : 0.f;
 #pragma unroll
-  for (int i = 0; i < V; ++i) most = fmaxf(most, fabsf(s[i]));
+  for (int i = 0; i < V; ++i)
+    if (!kInRange) most = fmaxf(most, fabsf(s[i]));
   // a NaN is dropped by fmaxf, but not by the sum: fp32 or 64 bits, it comes through
   if (most < 0x1p60f && (most > 0x1p-40f || most == 0.f)) {
     float q = 0.f;
@@ -144,17 +176,17 @@ __device__ __forceinline__ Clip clip_from_partials(const double *partials, int c
   return clip_of(block_sum(q, shared), max_norm);
 }
 
-template <class Args>
-__global__ void __launch_bounds__(kGradThreads) k_grad_squares(const __grid_constant__ Args a, double *partials) {
+template <class Args, bool kMore>
+__global__ void __launch_bounds__(kGradThreads, kMore ? 3 : 4) k_grad_squares(const __grid_constant__ Args a, double *partials) {
   __shared__ double shared[kGradThreads / 32];
   dependency_wait();
   double q = 0.0;
   for (uint32_t chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
     const GradEntry &t = a.t[entry_of(a, chunk)];
     auto one = [&](float s, uint64_t) { q = fma((double)s, (double)s, q); };
-    if (t.dtype == GS_TYPE_F32) chunk_sums<float>(a, t, chunk, [&](const float *s, uint64_t) { q += squares<4>(s); }, one);
-    else if (t.dtype == GS_TYPE_F16) chunk_sums<__half>(a, t, chunk, [&](const float *s, uint64_t) { q += squares<8>(s); }, one);
-    else chunk_sums<__nv_bfloat16>(a, t, chunk, [&](const float *s, uint64_t) { q += squares<8>(s); }, one);
+    if (t.dtype == GS_TYPE_F32) chunk_sums<float, kMore>(a, t, chunk, [&](const float *s, uint64_t) { q += squares<4>(s); }, one);
+    else if (t.dtype == GS_TYPE_F16) chunk_sums<__half, kMore>(a, t, chunk, [&](const float *s, uint64_t) { q += squares<8, !kMore>(s); }, one);   // (2^-48 to 2^32)
+    else chunk_sums<__nv_bfloat16, kMore>(a, t, chunk, [&](const float *s, uint64_t) { q += squares<8>(s); }, one);
   }
   q = block_sum(q, shared);
   if (threadIdx.x == 0) partials[blockIdx.x] = q;
@@ -167,12 +199,12 @@ __global__ void __launch_bounds__(kGradThreads) k_grad_norm(const double *partia
   if (threadIdx.x == 0) { clip[0] = c.norm; clip[1] = c.scale; }
 }
 
-template <class T, class Args>
+template <class T, bool kMore, class Args>
 __device__ __forceinline__ void scale_chunk(const Args &a, const GradEntry &t, uint32_t chunk, float scale) {
   constexpr int V = kVecOf<T>;
   T *out = static_cast<T *>(t.out);
   if (scale == 1.f && t.out == t.grad && t.num_more == 0) return;
-  chunk_sums<T>(
+  chunk_sums<T, kMore>(
       a, t, chunk,
       [&](float *s, uint64_t e) {
 #pragma unroll
@@ -181,18 +213,20 @@ __device__ __forceinline__ void scale_chunk(const Args &a, const GradEntry &t, u
       },
       [&](float s, uint64_t e) { out[e] = narrow<T>(scale > 0.f ? s * scale : 0.f); });
 }
-template <class Args>
-__global__ void __launch_bounds__(kGradThreads) k_grad_scale(const __grid_constant__ Args a, const double *partials, int count, float max_norm,
+template <class Args, bool kMore>
+__global__ void __launch_bounds__(kGradThreads, kMore ? 3 : 4) k_grad_scale(const __grid_constant__ Args a, const double *partials, int count, float max_norm,
                                                              float *clip) {
   __shared__ double shared[kGradThreads / 32];
   dependency_wait();
   const Clip c = clip_from_partials(partials, count, max_norm, shared);
   if (blockIdx.x == 0 && threadIdx.x == 0) { clip[0] = c.norm; clip[1] = c.scale; }
-  for (uint32_t chunk = blockIdx.x; chunk < a.chunks; chunk += gridDim.x) {
+  // from the end on: what the norm has read last is in the L2
+  for (uint32_t back = blockIdx.x; back < a.chunks; back += gridDim.x) {
+    const uint32_t chunk = a.chunks - 1 - back;
     const GradEntry &t = a.t[entry_of(a, chunk)];
-    if (t.dtype == GS_TYPE_F32) scale_chunk<float>(a, t, chunk, c.scale);
-    else if (t.dtype == GS_TYPE_F16) scale_chunk<__half>(a, t, chunk, c.scale);
-    else scale_chunk<__nv_bfloat16>(a, t, chunk, c.scale);
+    if (t.dtype == GS_TYPE_F32) scale_chunk<float, kMore>(a, t, chunk, c.scale);
+    else if (t.dtype == GS_TYPE_F16) scale_chunk<__half, kMore>(a, t, chunk, c.scale);
+    else scale_chunk<__nv_bfloat16, kMore>(a, t, chunk, c.scale);
   }
 }
 
@@ -218,10 +252,10 @@ int run(const GsGradTensor *tensors, int num_tensors, bool scale, float max_norm
     d.head = !same ? 0xffffffffu : (uint32_t)(head < d.count ? head : d.count);
     a.chunks += (uint32_t)((d.count + kGradChunk - 1) / kGradChunk);
   }
-  const uint32_t most = (uint32_t)(num_sms * 8 < kGradPartials ? num_sms * 8 : kGradPartials);
+  const uint32_t wave = (uint32_t)num_sms * (more ? 3u : 4u), most = wave < (uint32_t)kGradPartials ? wave : (uint32_t)kGradPartials;
   const uint32_t grid = a.chunks < most ? (a.chunks ? a.chunks : 1u) : most;
-  launch_chained(k_grad_squares<Args>, grid, kGradThreads, 0, st, a, partials);
-  if (scale) launch_chained(k_grad_scale<Args>, grid, kGradThreads, 0, st, a, (const double *)partials, (int)grid, max_norm, clip);
+  launch_chained(more ? k_grad_squares<Args, true> : k_grad_squares<Args, false>, grid, kGradThreads, 0, st, a, partials);
+  if (scale) launch_chained(more ? k_grad_scale<Args, true> : k_grad_scale<Args, false>, grid, kGradThreads, 0, st, a, (const double *)partials, (int)grid, max_norm, clip);
   else launch_chained(k_grad_norm, 1, kGradThreads, 0, st, (const double *)partials, (int)grid, max_norm, clip);
   return 2;
 }
@@ -232,7 +266,7 @@ int run(const GsGradTensor *tensors, int num_tensors, bool scale, float max_norm
 int launch_grad_clip(const GsGradTensor *tensors, int num_tensors, bool scale, float max_norm, float *clip, double *partials, int num_sms, cudaStream_t st) {
   int more = 0;
   for (int i = 0; i < num_tensors; ++i) more += tensors[i].num_more_grads;
-  if (num_tensors <= 24 && more <= 64) return run<GradArgsSmall>(tensors, num_tensors, scale, max_norm, clip, partials, num_sms, st);
+  if (num_tensors <= 64 && more <= 128) return run<GradArgsSmall>(tensors, num_tensors, scale, max_norm, clip, partials, num_sms, st);
   return run<GradArgsLarge>(tensors, num_tensors, scale, max_norm, clip, partials, num_sms, st);
 }
 
