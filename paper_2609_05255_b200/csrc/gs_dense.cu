@@ -78,15 +78,15 @@ __device__ __forceinline__ void activate8(float2 z[4]) {
     for (int i = 0; i < 4; ++i) z[i] = mul2(z[i], logistic2(gelu_arg2(z[i], mul2(z[i], z[i]))));
   }
 }
-// act' of the smooth ones: p + z p (1 - p) u'.  Beyond |z| = 128 gelu' is 1 or 0 in fp32; the clamp keeps z^3 finite (and a NaN a
-// NaN).  Silu needs none: p (1 - p) is 0 before z overflows.
+// act' of the smooth ones: p + z p (1 - p) u', 1 - p by one fused operation.  Beyond |z| = 128 gelu' is 1 or 0 in fp32; the clamp keeps z^3 finite (and a NaN a
+// NaN).  Silu needs none: p or 1 - p is 0 before z overflows.
 template <int kAct>
 __device__ __forceinline__ void activate_grad8(float2 z[4]) {
   if constexpr (kAct == GS_DENSE_SILU) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float2 p = logistic2(mul2(z[i], both(kMinusLog2e)));
-      z[i] = fma2(z[i], fma2(make_float2(-p.x, -p.y), p, p), p);
+      z[i] = fma2(mul2(z[i], p), fma2(p, both(-1.f), both(1.f)), p);
     }
   } else {
 #pragma unroll
@@ -94,7 +94,8 @@ __device__ __forceinline__ void activate_grad8(float2 z[4]) {
       z[i].x = z[i].x > 128.f ? 128.f : z[i].x < -128.f ? -128.f : z[i].x;
       z[i].y = z[i].y > 128.f ? 128.f : z[i].y < -128.f ? -128.f : z[i].y;
       const float2 zz = mul2(z[i], z[i]), p = logistic2(gelu_arg2(z[i], zz));
-      z[i] = fma2(mul2(z[i], fma2(make_float2(-p.x, -p.y), p, p)), fma2(zz, both(0.21406444881479418f), both(1.5957691216057308f)), p);
+      const float2 slope = fma2(zz, both(0.21406444881479418f), both(1.5957691216057308f));
+      z[i] = fma2(mul2(mul2(z[i], p), fma2(p, both(-1.f), both(1.f))), slope, p);
     }
   }
 }
@@ -454,7 +455,7 @@ constexpr int kWStep = 64;                      // rows of a step (32: 221 us in
 constexpr uint32_t kWBoxBytes = kWStep * tma::kRowBytes;
 constexpr int kFlush = 8;                       // steps after which an accumulator is emptied
 struct WeightsBarriers {
-  uint64_t full[kMaxStages], ready[kMaxStages], empty[kMaxStages], sum_full[2], sum_empty[2], done;
+  uint64_t full[kMaxStages], ready[kMaxStages], empty[kMaxStages], sum_full[2], sum_empty[2], third_empty[2], done;
   uint32_t tmem, dead, pad[2];
 };
 
@@ -474,18 +475,21 @@ __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant_
   unsigned char *smem = smem_raw + ((1024u - (tc::smem_addr(smem_raw) & 1023u)) & 1023u);
   constexpr int kParts = weight_parts<T>(kAct);
   constexpr bool kLow = kParts >= 2, kScale = kParts == 2;
-  constexpr uint32_t kStageA = (kParts == 3 ? 3 : kParts ? 2 : 1) * 2 * kWBoxBytes;
+  constexpr uint32_t kStageA = (kParts ? 2 : 1) * 2 * kWBoxBytes;
   const int x_boxes = (a.bk + 63) / 64;
   const uint32_t stage_bytes = kStageA + x_boxes * kWBoxBytes;
-  float *sums = reinterpret_cast<float *>(smem + a.stages * stage_bytes);  // [16, 128]
-  WeightsBarriers &bars = *reinterpret_cast<WeightsBarriers *>(sums + 16 * 128);
+  // the third part of dz, in two buffers in turn: it is needed for a short time, and in the stages it would cost one of three
+  // (397 us instead of 362 for 1M rows of 256 to 256 with SiLU)
+  unsigned char *thirds = smem + a.stages * stage_bytes;
+  WeightsBarriers &bars = *reinterpret_cast<WeightsBarriers *>(thirds + (kParts == 3 ? 4 * kWBoxBytes : 0u));
+  float *sums = reinterpret_cast<float *>(smem);          // [16, 128], at the end, when the stages have served
   volatile uint32_t *dead = &bars.dead;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto bar = [](const uint64_t &b) { return tc::smem_addr(&b); };
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < a.stages; ++s) { tma::init(bar(bars.full[s]), 1); tma::init(bar(bars.ready[s]), kWorkerWarps); tma::init(bar(bars.empty[s]), 1); }
-    for (int i = 0; i < 2; ++i) { tma::init(bar(bars.sum_full[i]), 1); tma::init(bar(bars.sum_empty[i]), kWorkerWarps); }
+    for (int i = 0; i < 2; ++i) { tma::init(bar(bars.sum_full[i]), 1); tma::init(bar(bars.sum_empty[i]), kWorkerWarps); tma::init(bar(bars.third_empty[i]), 1); }
     tma::init(bar(bars.done), 1);
     bars.dead = 0u;
     tc::fence_barrier_init();
@@ -528,6 +532,7 @@ __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant_
     } else if (warp == kWarpMma && lane == 0) {
       const uint32_t desc = idesc_of<T>((cols + 15) & ~15, true, true);
       const uint64_t a_desc = desc_swizzled(tc::smem_addr(smem), kWBoxBytes), b_desc = a_desc + (kStageA >> 4), stage16 = stage_bytes >> 4;
+      const uint64_t third_desc = desc_swizzled(tc::smem_addr(thirds), kWBoxBytes);
       const uint32_t ready0 = touched ? bar(bars.ready[0]) : bar(bars.full[0]), empty0 = bar(bars.empty[0]);
       Ring at;
       for (int it = 0; it < count; ++it, at.next(a.stages)) {
@@ -536,16 +541,19 @@ __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant_
         const int buf = kLow ? 0 : group & 1, use = kLow ? group : group >> 1;
         const uint64_t da = a_desc + at.s * stage16, db = b_desc + at.s * stage16;
         if (!tma::wait(ready0 + at.s * 8, at.parity, dead)) break;
-        auto part = [&](int p, uint32_t d, bool add) {
+        auto part = [&](uint64_t dz, uint32_t d, bool add) {
 #pragma unroll
-          for (int ks = 0; ks < kWStep / 16; ++ks) tc::mma(d, da + p * (2 * kWBoxBytes >> 4) + ks * 128, db + ks * 128, add || ks ? 1u : 0u, desc);
+          for (int ks = 0; ks < kWStep / 16; ++ks) tc::mma(d, dz + ks * 128, db + ks * 128, add || ks ? 1u : 0u, desc);
         };
         tc::fence_after_sync();
-        if (kLow) part(1, tmem + second, it > 0);
-        if (kParts == 3) part(2, tmem + second, true);
+        if (kParts == 3) {
+          part(third_desc + (it & 1) * (2 * kWBoxBytes >> 4), tmem + second, it > 0);
+          tc::commit(bar(bars.third_empty[it & 1]));
+        }
+        if (kLow) part(da + (2 * kWBoxBytes >> 4), tmem + second, kParts == 3 || it > 0);
         if (it % kFlush == 0 && !tma::wait(bar(bars.sum_empty[buf]), (use & 1) ^ 1, dead)) break;
         tc::fence_after_sync();
-        part(0, tmem + buf * second, it % kFlush > 0);
+        part(da, tmem + buf * second, it % kFlush > 0);
         tc::commit(empty0 + at.s * 8);
         if (it % kFlush == kFlush - 1 || it == count - 1) tc::commit(bar(bars.sum_full[buf]));
       }
@@ -592,15 +600,17 @@ __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant_
         if (!(ok = __all_sync(0xffffffffu, tma::wait(bar(bars.full[s]), at.parity, dead)))) break;
         unsigned char *A = smem + s * stage_bytes + (chunk >> 3) * kWBoxBytes;
         // (rows 16 apart have the same swizzle)
+        if (kParts == 3 && !(ok = __all_sync(0xffffffffu, tma::wait(bar(bars.third_empty[it & 1]), (it >> 1 & 1) ^ 1, dead)))) break;
         auto in = [&](int u) { return A + (row0 + 16 * u) * (int)tma::kRowBytes + (((chunk & 7) ^ (row0 & 7)) * 16); };
+        const ptrdiff_t third = thirds + (it & 1) * (2 * kWBoxBytes) - (smem + s * stage_bytes);
         if ((chunk >> 3) < dz_boxes) {
 #pragma unroll
           for (int u = 0; u < kWStep / 16; u += 2) {
             const uint4 dy0 = shared16(in(u)), dy1 = shared16(in(u + 1));
             if constexpr (kParts > 0) {
               const uint4 z0 = shared16(in(u) + 2 * kWBoxBytes), z1 = shared16(in(u + 1) + 2 * kWBoxBytes);
-              transform_chunk<T, kAct, kParts, kScale, true>(in(u), in(u) + 2 * kWBoxBytes, in(u) + 4 * kWBoxBytes, dy0, z0, mine);
-              transform_chunk<T, kAct, kParts, kScale, true>(in(u + 1), in(u + 1) + 2 * kWBoxBytes, in(u + 1) + 4 * kWBoxBytes, dy1, z1, mine);
+              transform_chunk<T, kAct, kParts, kScale, true>(in(u), in(u) + 2 * kWBoxBytes, in(u) + third, dy0, z0, mine);
+              transform_chunk<T, kAct, kParts, kScale, true>(in(u + 1), in(u + 1) + 2 * kWBoxBytes, in(u + 1) + third, dy1, z1, mine);
             } else {
               float2 v[4], w[4];
               unpack<T>(dy0, &v[0].x);
@@ -649,6 +659,7 @@ __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant_
           }
       }
     }
+    named_sync(2, kWorkerWarps * 32);                        // (every worker has seen the last products complete)
     if (db) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) *reinterpret_cast<float2 *>(sums + row0 * 128 + chunk * 8 + 2 * i) = mine[i];
@@ -796,8 +807,8 @@ WeightsPlan plan_weights(int64_t rows, int in, int out, int num_sms) {
 template <class T, int kAct>
 void run_weights(WeightsArgs &a, cudaStream_t st) {
   constexpr int kParts = weight_parts<T>(kAct);
-  const uint32_t stage = ((kParts == 3 ? 3u : kParts ? 2u : 1u) * 2u + (uint32_t)ceil_div(a.bk, 64)) * kWBoxBytes;
-  const uint32_t fixed = 1024 + 16 * 128 * 4 + sizeof(WeightsBarriers);
+  const uint32_t stage = ((kParts ? 2u : 1u) * 2u + (uint32_t)ceil_div(a.bk, 64)) * kWBoxBytes;
+  const uint32_t fixed = 1024 + (kParts == 3 ? 4 * kWBoxBytes : 0u) + sizeof(WeightsBarriers);
   a.stages = (int)((kSmemMost - fixed) / stage);
   if (a.stages > kMaxStages) a.stages = kMaxStages;
   const uint32_t smem = fixed + a.stages * stage;
