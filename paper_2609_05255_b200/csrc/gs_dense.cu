@@ -78,9 +78,9 @@ __device__ __forceinline__ void activate8(float2 z[4]) {
     for (int i = 0; i < 4; ++i) z[i] = mul2(z[i], logistic2(gelu_arg2(z[i], mul2(z[i], z[i]))));
   }
 }
-// act' of the smooth ones: p + z p (1 - p) u', 1 - p by one fused operation.  Beyond |z| = 128 gelu' is 1 or 0 in fp32; the clamp keeps z^3 finite (and a NaN a
-// NaN).  Silu needs none: p or 1 - p is 0 before z overflows.
-template <int kAct>
+// act' of the smooth ones: p + z p (1 - p) u', 1 - p by one fused operation.  p or 1 - p is 0 before a product overflows, but for z^2 of
+// gelu in bf16 (kWide), which is held below 1e30; a NaN stays one.
+template <int kAct, bool kWide>
 __device__ __forceinline__ void activate_grad8(float2 z[4]) {
   if constexpr (kAct == GS_DENSE_SILU) {
 #pragma unroll
@@ -91,9 +91,9 @@ __device__ __forceinline__ void activate_grad8(float2 z[4]) {
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      z[i].x = z[i].x > 128.f ? 128.f : z[i].x < -128.f ? -128.f : z[i].x;
-      z[i].y = z[i].y > 128.f ? 128.f : z[i].y < -128.f ? -128.f : z[i].y;
-      const float2 zz = mul2(z[i], z[i]), p = logistic2(gelu_arg2(z[i], zz));
+      float2 zz = mul2(z[i], z[i]);
+      if (kWide) zz = make_float2(fminf(zz.x, 1e30f), fminf(zz.y, 1e30f));
+      const float2 p = logistic2(gelu_arg2(z[i], zz));
       const float2 slope = fma2(zz, both(0.21406444881479418f), both(1.5957691216057308f));
       z[i] = fma2(mul2(mul2(z[i], p), fma2(p, both(-1.f), both(1.f))), slope, p);
     }
@@ -136,7 +136,7 @@ __device__ __forceinline__ void transform_chunk(unsigned char *a, unsigned char 
   uint32_t *dw = &dy.x, *zw = &z.x, *tw = &third.x;
   float2 g[4];
   unpack<T>(z, &g[0].x);
-  if constexpr (kParts > 1) activate_grad8<kAct>(g);
+  if constexpr (kParts > 1) activate_grad8<kAct, !__is_same(T, __half)>(g);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 d = widen2<T>(dw[i]);
