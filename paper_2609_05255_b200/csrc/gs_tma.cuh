@@ -1,5 +1,5 @@
 // Tiled copies by the tensor memory accelerator, and waits for them.  Included inside namespace gs's unnamed namespace after
-// gs_tcgen05.cuh, by translation units that include <cuda.h>.  Single-GPU code: no cluster, no multicast.
+// gs_tcgen05.cuh, by translation units that include <cuda.h>.  Copies go to the CTA that issues them, never to others of a cluster.
 //
 // A matrix of 16-bit values, row-major with rows `ld` elements apart, is copied in boxes of 64 columns (128 bytes: the span
 // of the 128-byte swizzle, which moves the 16-byte chunk c of a row r of the box to c ^ (r mod 8)) and a number of rows.  What a box
@@ -50,18 +50,25 @@ __device__ __forceinline__ void expect(uint32_t bar, uint32_t bytes) {
 }
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+// kCluster: what the other CTA of a cluster wrote before it arrived is visible, too.
+template <bool kCluster = false>
 __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
   uint32_t done;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  if (kCluster)
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
   return done != 0;
 }
 // Waits for a phase, at most 2^32 cycles (about two seconds) or until another role of the CTA has given up.  Who gives up says so
 // in *dead: everybody's waits then end, and the CTA leaves in order.
+template <bool kCluster = false>
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile uint32_t *dead) {
-  if (try_wait(bar, parity)) return true;
+  if (try_wait<kCluster>(bar, parity)) return true;
   const long long begin = clock64();
-  while (!try_wait(bar, parity)) {
+  while (!try_wait<kCluster>(bar, parity)) {
     if (*dead) return false;
     if (clock64() - begin > (1ll << 32)) {
       *dead = 1u;
