@@ -686,6 +686,20 @@ __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant_
       if (it % kFlush == 0 && it > 0) flush(it / kFlush - 1);
     }
     if (ok && count > 0) flush((count - 1) / kFlush);
+    if constexpr (kLow) {
+      // (all products have completed with the last group's: the high part's are issued last)
+      if (ok && count > 0) {
+#pragma unroll
+        for (int c = 0; c < 128; c += 32)
+          if (half * 128 + c < cols) {
+            float v[32];
+            load32(lanes + second + c, v);
+            constexpr float k = kScale ? 1.f / 2048.f : 1.f;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) acc[c + i] = fmaf(v[i], k, acc[c + i]);
+          }
+      }
+    }
     if (ok && n < a.n) {
       float *out = a.partials + ((size_t)split * a.n + n) * a.ld + k0 + half * 128;
 #pragma unroll
@@ -695,28 +709,6 @@ __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant_
           for (int i = 0; i < 32; i += 4)
             if (half * 128 + c + i < cols) *reinterpret_cast<float4 *>(out + c + i) = make_float4(acc[c + i], acc[c + i + 1], acc[c + i + 2], acc[c + i + 3]);
         }
-    }
-    if constexpr (kLow) {
-      // (all products have completed with the last group's: the high part's are issued last)
-      if (__any_sync(0xffffffffu, ok && count > 0 && n < a.n)) {
-        float *out = a.partials + ((size_t)split * a.n + n) * a.ld + k0 + half * 128;
-#pragma unroll
-        for (int c = 0; c < 128; c += 32)
-          if (half * 128 + c < cols) {
-            float v[32];
-            load32(lanes + second + c, v);
-            if (n < a.n) {
-#pragma unroll
-              for (int i = 0; i < 32; i += 4)
-                if (half * 128 + c + i < cols) {
-                  float4 w = *reinterpret_cast<const float4 *>(out + c + i);
-                  constexpr float k = kScale ? 1.f / 2048.f : 1.f;
-                  w.x = fmaf(v[i], k, w.x); w.y = fmaf(v[i + 1], k, w.y); w.z = fmaf(v[i + 2], k, w.z); w.w = fmaf(v[i + 3], k, w.w);
-                  *reinterpret_cast<float4 *>(out + c + i) = w;
-                }
-            }
-          }
-      }
     }
     named_sync(2, kWorkerWarps * 32);                        // (every worker has seen the last products complete)
     if (db) {
@@ -739,21 +731,55 @@ __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant_
   if (warp == kWarpMma) tc::tmem_free(tmem, a.tmem_cols);
 }
 
-// dW [n, k] and db [n] from the splits' sums, added in their order.
-__global__ void __launch_bounds__(256) k_dense_sums(const float *partials, const float *db_partials, int splits, int n, int k, int ld, float *dw, float *db) {
+// dW [n, k] and db [n] from the splits' sums, four values a lane.  Many splits are taken by 16 groups of lanes, so that many loads are in
+// flight (256 to 8 with 148 splits: the weights' gradient 35 us instead of 39), whose sums are added in their order; few
+// by one (1024 to 1024 with 4: 61 instead of 87).  The last CTAs take db.
+template <int kGroups>
+__global__ void __launch_bounds__(512) k_dense_sums(const float *partials, const float *db_partials, int splits, int n, int k, int ld, int blocks, float *dw, float *db) {
+  constexpr int kLanes = 512 / kGroups, kValues = 4 * kLanes;
+  __shared__ double part[kGroups > 1 ? kGroups : 1][kGroups > 1 ? kValues : 1];
   dependency_wait();
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, count = (int64_t)n * ld, stride = count;
-  if (i < count) {
-    const int row = (int)(i / ld), col = (int)(i % ld);
-    if (col < k) {
-      double s = 0.0;
-      for (int p = 0; p < splits; ++p) s += (double)__ldcs(partials + p * stride + i);
-      dw[(int64_t)row * k + col] = (float)s;
+  const bool bias = (int)blockIdx.x >= blocks;
+  const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+  const int64_t count = bias ? n : (int64_t)n * ld, first = (int64_t)(bias ? blockIdx.x - blocks : blockIdx.x) * kValues;
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  if (!bias) {
+    const int64_t i = first + lane * 4;                       // (rows of partial sums are a multiple of four values)
+    if (i < count) {
+#pragma unroll 4
+      for (int p = group; p < splits; p += kGroups) {
+        const float4 v = __ldcs(reinterpret_cast<const float4 *>(partials + p * count + i));
+        s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+      }
     }
-  } else if (db && i - count < n) {
-    double s = 0.0;
-    for (int p = 0; p < splits; ++p) s += (double)__ldcs(db_partials + (int64_t)p * n + (i - count));
-    db[i - count] = (float)s;
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (first + lane * 4 + q < count)
+        for (int p = group; p < splits; p += kGroups) s[q] += __ldcs(db_partials + p * count + first + lane * 4 + q);
+  }
+  auto put = [&](int64_t i, double v) {
+    if (i >= count) return;
+    if (bias) {
+      db[i] = (float)v;
+    } else {
+      const int row = (int)(i / ld), col = (int)(i % ld);
+      if (col < k) dw[(int64_t)row * k + col] = (float)v;
+    }
+  };
+  if constexpr (kGroups == 1) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) put(first + lane * 4 + q, s[q]);
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) part[group][lane * 4 + q] = s[q];
+    __syncthreads();
+    if (threadIdx.x < kValues) {
+      double t = part[0][threadIdx.x];
+#pragma unroll
+      for (int g = 1; g < kGroups; ++g) t += part[g][threadIdx.x];
+      put(first + threadIdx.x, t);
+    }
   }
 }
 
@@ -773,7 +799,8 @@ bool shape_rows(RowsArgs &a, bool forward, bool transform, int bn, int ctas, boo
   a.resident = resident;
   const uint32_t stage = (transform ? 2 : 1) * kTileBytes + (resident ? 0u : a.b_bytes);
   const uint64_t fixed = 1024 + 1024 + sizeof(RowsBarriers) + (resident ? (uint64_t)a.k_blocks * a.b_bytes : 0u);
-  for (a.out_slots = 4; a.out_slots >= 2; a.out_slots -= 2) {
+  // (where the weights come with every step, a step more before a tile more on its way out: 20 011 rows of 1024 to 1024 50 us instead of 55)
+  for (a.out_slots = resident ? 4 : 2; a.out_slots >= 2; a.out_slots -= 2) {
     a.keep_slots = !a.has_keep ? 0 : a.has_residual ? 2 : a.out_slots;
     const uint64_t used = fixed + (uint64_t)(a.out_slots + a.keep_slots) * kTileBytes;
     if (used + (uint64_t)want * stage > kSmemMost) continue;
@@ -931,8 +958,13 @@ int bwd(const DenseArgs &d, int num_sms, cudaStream_t st) {
     else if (d.act == GS_DENSE_RELU) run_weights<T, GS_DENSE_RELU>(a, st);
     else if (d.act == GS_DENSE_SILU) run_weights<T, GS_DENSE_SILU>(a, st);
     else run_weights<T, GS_DENSE_GELU>(a, st);
-    launch_chained(k_dense_sums, ceil_div((int64_t)d.out * p.ld + (d.db ? d.out : 0), 256), 256, 0, st, (const float *)a.partials,
-                   (const float *)a.db_partials, p.splits, d.out, d.in, p.ld, d.dw, d.db);
+    auto sum = [&](auto kernel, int values) {
+      const int blocks = ceil_div((int64_t)d.out * p.ld, values);
+      launch_chained(kernel, blocks + (d.db ? ceil_div(d.out, values) : 0), 512, 0, st, (const float *)a.partials, (const float *)a.db_partials, p.splits, d.out, d.in,
+                     p.ld, blocks, d.dw, d.db);
+    };
+    if (p.splits >= 16) sum(k_dense_sums<16>, 128);
+    else sum(k_dense_sums<1>, 2048);
     launches += 2;
   }
   return launches;
