@@ -799,7 +799,7 @@ bool shape_rows(RowsArgs &a, bool forward, bool transform, int bn, int ctas, boo
   a.resident = resident;
   const uint32_t stage = (transform ? 2 : 1) * kTileBytes + (resident ? 0u : a.b_bytes);
   const uint64_t fixed = 1024 + 1024 + sizeof(RowsBarriers) + (resident ? (uint64_t)a.k_blocks * a.b_bytes : 0u);
-  // (where the weights come with every step, a step more before a tile more on its way out: 20 011 rows of 1024 to 1024 50 us instead of 55)
+  // (where the weights come with every step, a step more before a tile more on its way out: 20 011 rows of 1024 to 1024 41.7 us instead of 44.2)
   for (a.out_slots = resident ? 4 : 2; a.out_slots >= 2; a.out_slots -= 2) {
     a.keep_slots = !a.has_keep ? 0 : a.has_residual ? 2 : a.out_slots;
     const uint64_t used = fixed + (uint64_t)(a.out_slots + a.keep_slots) * kTileBytes;
@@ -824,9 +824,12 @@ int plan_rows(RowsArgs &a, bool forward, bool transform, int num_sms, uint32_t &
   // instead of 287.  Without dz the steps are small and the first CTA's wait for both costs more than it brings: 181 instead of
   // 164, forward with residual 350 instead of 313, 20 011 rows of 1024 to 1024 55 instead of 50.
   if (transform && bn > 128 && a.m_tiles >= 2 && shape_rows(a, forward, transform, 256, 2, true, 3, smem)) ctas = 2;
-  // Else resident weights, rather of a narrower tile than not; then a pipeline of three steps.
-  if (ctas == 1 && !(shape_rows(a, forward, transform, bn, 1, true, 3, smem) || shape_rows(a, forward, transform, narrow, 1, true, 3, smem) ||
-                     shape_rows(a, forward, transform, bn, 1, false, 3, smem) || shape_rows(a, forward, transform, narrow, 1, false, 2, smem)))
+  // Else resident weights, up to six steps of a narrower tile if need be (forward, 300 000 rows of 256 to 256 with residual and kept
+  // pre-activation 103 us instead of 153; 100 000 of 320 to 512 85 instead of 110), beyond that weights that come with every step
+  // rather than two looks at the rows (100 000 of 512 to 512 65 instead of 83).
+  if (ctas == 1 && !(shape_rows(a, forward, transform, bn, 1, true, 3, smem) || (a.k_blocks <= 6 && shape_rows(a, forward, transform, narrow, 1, true, 3, smem)) ||
+                     shape_rows(a, forward, transform, bn, 1, false, 3, smem) || shape_rows(a, forward, transform, narrow, 1, true, 3, smem) ||
+                     shape_rows(a, forward, transform, narrow, 1, false, 2, smem)))
     return 0;
   a.tmem_cols = tmem_columns(2u * (((uint32_t)a.bn + 63u) & ~63u));
   const int tiles = ceil_div(a.m_tiles, ctas);
