@@ -7,7 +7,8 @@
 // lives in the registers of a group of lanes (1 to 32 of a warp, or the 256 of a CTA), as the vectors of 16 bytes it was
 // loaded in; the variance is taken about the mean in a second pass over the registers, which loses nothing where the mean is
 // large against the spread.  All sums in fp32, two operations an instruction (add2 and the like): with one each the arithmetic
-// was the bound (1M rows of 256 took 349 us forward, 432 backward; together with the row fetched ahead 189 and 282).  The grid is persistent: a lane keeps its columns from row to row, so
+// was the bound (1M rows of 256 took 349 us forward, 432 backward; together with the row fetched ahead, the exchanges
+// written out and running pointers 179 and 276, 88 and 85 % of the copy rate).  The grid is persistent: a lane keeps its columns from row to row, so
 // gamma and beta stay in registers, and in the backward so do its sums for dgamma and dbeta, which leave as one row of partial
 // sums per CTA and are added up by k_layer_norm_sums in a fixed order (no atomics: the same bits from run to run).
 #include <cuda_bf16.h>
@@ -25,7 +26,7 @@ constexpr int kNormPartialRows = 592;     // most CTAs of the backward
 
 // CTAs per SM, of as many registers as the elements of a lane need, and no more CTAs than are resident: 1M rows of 256 in bf16
 // forward 189 us with three, 221 with four (spills), 308 with two; backward in fp16 282 with two, 324 with the compiler's choice.
-__host__ __device__ constexpr int fwd_ctas(int elements) { return elements <= 8 ? 6 : elements <= 16 ? 3 : 1; }
+__host__ __device__ constexpr int fwd_ctas(int elements) { return elements <= 8 ? 4 : elements <= 16 ? 3 : 1; }
 __host__ __device__ constexpr int bwd_ctas(int elements) { return elements <= 8 ? 3 : elements <= 16 ? 2 : 1; }
 
 // How a row is laid over lanes: `lanes` of them with NV vectors of V elements each, vector j of lane l at column (j lanes + l) V.
@@ -79,11 +80,12 @@ __device__ __forceinline__ void put(T *p, int lane, int lanes, int cols, const f
   }
 }
 
-// Sums over a group; the same in every lane.
+// Sums over a group; the same in every lane.  (The steps are written out: a loop over them was a third of a row's instructions.)
 template <bool kBlock>
 __device__ __forceinline__ float2 group_sum2(float2 v, int lanes, float2 *shared) {
-  for (int o = (kBlock ? 32 : lanes) >> 1; o > 0; o >>= 1)
-    v = add2(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    if (kBlock || lanes > o) v = add2(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
   if constexpr (kBlock) {
     __syncthreads();
     if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = v;
@@ -99,7 +101,9 @@ __device__ __forceinline__ float group_sum(float v, int lanes, float2 *shared) {
   if constexpr (kBlock) {
     return group_sum2<true>(make_float2(v, 0.f), lanes, shared).x;
   } else {
-    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+      if (lanes > o) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
   }
 }
@@ -133,11 +137,15 @@ __global__ void __launch_bounds__(kNormThreads, fwd_ctas(V * NV)) k_layer_norm_f
   const int64_t step = (int64_t)gridDim.x * groups;
   int64_t row = (int64_t)blockIdx.x * groups + group;
   Row<T, V, NV> x;
-  x.load(static_cast<const T *>(a.x) + row * a.ld_x, lane, lanes, a.cols, row < a.rows);
-  for (int64_t row0 = (int64_t)blockIdx.x * groups; row0 < a.rows; row0 += step, row += step) {
+  const T *from = static_cast<const T *>(a.x) + row * a.ld_x;
+  T *to = static_cast<T *>(a.y) + row * a.ld_out;
+  const int64_t from_step = step * a.ld_x, to_step = step * a.ld_out;
+  x.load(from, lane, lanes, a.cols, row < a.rows);
+  for (int64_t row0 = (int64_t)blockIdx.x * groups; row0 < a.rows; row0 += step, row += step, to += to_step) {
     float2 v[P];
     x.get(v);
-    x.load(static_cast<const T *>(a.x) + (row + step) * a.ld_x, lane, lanes, a.cols, row + step < a.rows);
+    from += from_step;
+    x.load(from, lane, lanes, a.cols, row + step < a.rows);
     float2 s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < P; ++i) s = add2(s, v[i]);
@@ -153,11 +161,11 @@ __global__ void __launch_bounds__(kNormThreads, fwd_ctas(V * NV)) k_layer_norm_f
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) s = fma2(v[i], v[i], s);
-    const float rstd = 1.f / sqrtf(fmaf(group_sum<kBlock>(s.x + s.y, lanes, shared), inv, a.eps));
+    const float rstd = rsqrtf(fmaf(group_sum<kBlock>(s.x + s.y, lanes, shared), inv, a.eps));
     if (row < a.rows) {
 #pragma unroll
       for (int i = 0; i < P; ++i) v[i] = fma2(mul2(v[i], both(rstd)), gamma[i], beta[i]);
-      put<T, V, NV>(static_cast<T *>(a.y) + row * a.ld_out, lane, lanes, a.cols, v);
+      put<T, V, NV>(to, lane, lanes, a.cols, v);
       if (lane == 0) {
         if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;
@@ -182,15 +190,19 @@ __global__ void __launch_bounds__(kNormThreads, bwd_ctas(V * NV)) k_layer_norm_b
   int64_t row = (int64_t)blockIdx.x * groups + group;
   Row<T, V, NV> x, dy;
   float mean, rstd;
+  const T *from_x = static_cast<const T *>(a.x) + row * a.ld_x, *from_dy = static_cast<const T *>(a.dy) + row * a.ld_dy;
+  T *to = a.dx ? static_cast<T *>(a.dx) + row * a.ld_out : nullptr;
+  const int64_t x_step = step * a.ld_x, dy_step = step * a.ld_dy, to_step = a.dx ? step * a.ld_out : 0;
   auto fetch = [&](int64_t r) {
     const bool live = r < a.rows;
-    x.load(static_cast<const T *>(a.x) + r * a.ld_x, lane, lanes, a.cols, live);
-    dy.load(static_cast<const T *>(a.dy) + r * a.ld_dy, lane, lanes, a.cols, live);
+    x.load(from_x, lane, lanes, a.cols, live);
+    dy.load(from_dy, lane, lanes, a.cols, live);
+    from_x += x_step; from_dy += dy_step;
     mean = live ? __ldg(a.mean + r) : 0.f;
     rstd = live ? __ldg(a.rstd + r) : 0.f;
   };
   fetch(row);
-  for (int64_t row0 = (int64_t)blockIdx.x * groups; row0 < a.rows; row0 += step, row += step) {
+  for (int64_t row0 = (int64_t)blockIdx.x * groups; row0 < a.rows; row0 += step, row += step, to += to_step) {
     float2 h[P], g[P];
     x.get(h);
     dy.get(g);
@@ -214,7 +226,7 @@ __global__ void __launch_bounds__(kNormThreads, bwd_ctas(V * NV)) k_layer_norm_b
       const float2 avg_g = both(-sums.x * inv), avg_gh = both(-sums.y * inv);
 #pragma unroll
       for (int i = 0; i < P; ++i) g[i] = mul2(add2(fma2(h[i], avg_gh, g[i]), avg_g), r);
-      put<T, V, NV>(static_cast<T *>(a.dx) + row * a.ld_out, lane, lanes, a.cols, g);
+      put<T, V, NV>(to, lane, lanes, a.cols, g);
     }
   }
   if constexpr (kParams) {
