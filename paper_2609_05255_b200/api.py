@@ -637,17 +637,22 @@ def gs_dense_workspace_bytes(rows: int, in_features: int, out_features: int) -> 
     return int(_lib.gs_dense_workspace_bytes(rows, in_features, out_features))
 
 
-def _on(ctx: Context, layer: DenseLayer):
-    if layer.weight.device != ctx.device:
-        _invalid(f"the layer's weight is on {layer.weight.device}, the context on {ctx.device}")
+def _layer(ctx: Context, layer: DenseLayer) -> GsDenseLayer:
+    """The layer's struct with the addresses that its tensors have now."""
+    s, w = layer._struct, layer.weight
+    if w.device != ctx.device or w.shape != (s.out_features, s.in_features):
+        _invalid(f"the layer's weight is {list(w.shape)} on {w.device}, the layer made for [{s.out_features}, {s.in_features}], the context on {ctx.device}")
+    s.weight, s.ld_weight = w.data_ptr(), w.stride(0) if s.out_features > 1 else (s.in_features + 7) // 8 * 8
+    if layer.bias is not None:
+        s.bias = _vector(ctx, layer.bias, "bias", s.out_features)
+    return s
 
 
 def gs_dense_forward(ctx: Context, layer: DenseLayer, x: torch.Tensor, y: torch.Tensor, preact: Optional[torch.Tensor] = None,
                      residual: Optional[torch.Tensor] = None, stream=None) -> None:
     """y = act(x W^T + bias) + residual; preact receives x W^T + bias.  Matrices in the weight's type, rows a multiple of eight
     elements apart; residual may be y."""
-    _on(ctx, layer)
-    s, dt, rows = layer._struct, layer.weight.dtype, x.shape[0]
+    s, dt, rows = _layer(ctx, layer), layer.weight.dtype, x.shape[0]
     n = s.out_features
     px, lx = _matrix(ctx, x, "x", rows, s.in_features, dt)
     pr, lr = _matrix(ctx, residual, "residual", rows, n, dt)
@@ -662,8 +667,7 @@ def gs_dense_backward(ctx: Context, layer: DenseLayer, x: Optional[torch.Tensor]
                       workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """Gradients of gs_dense_forward; what is None is left out.  dL_dx in the weight's type, dL_dweight [out, in] and dL_dbias
     [out] float32.  preact is needed by a layer with an activation, workspace (gs_dense_workspace_bytes) and x by dL_dweight."""
-    _on(ctx, layer)
-    s, dt, rows = layer._struct, layer.weight.dtype, dL_dy.shape[0]
+    s, dt, rows = _layer(ctx, layer), layer.weight.dtype, dL_dy.shape[0]
     n, k = s.out_features, s.in_features
     px, lx = _matrix(ctx, x, "x", rows, k, dt)
     pz, lz = _matrix(ctx, preact, "preact", rows, n, dt)
@@ -724,7 +728,8 @@ class GradTensor:
 
 
 class GradList:
-    """The gradients of a model, marshalled once for the calls of every iteration."""
+    """The gradients of a model, marshalled once for the calls of every iteration: the buffers' addresses are taken here, so a list is
+    made anew when a buffer has got other memory (their values may change)."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)              # kept alive

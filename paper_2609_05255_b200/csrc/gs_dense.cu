@@ -527,7 +527,7 @@ __host__ __device__ constexpr int weight_parts(int act) {
 // The tensor core cuts off what an addition leaves below the accumulator's last bit, so over thousands of additions the sums
 // shrink: 1M rows in 74 splits were 9e-5 off.  So the accumulator of dz, or of its high part, is emptied every 8 steps, after
 // 32 additions, into fp32 registers of the eight worker warps, which round to nearest (two accumulators in turn where there
-// is one part: 4e-7 off).  The other parts have an accumulator of their own, which loses as much of 2^-8 as much.
+// is one part: 2e-7 to 7e-7 off).  The other parts have an accumulator of their own, which loses as much of 2^-8 as much.
 template <class T, int kAct>
 __global__ void __launch_bounds__(384, 1) k_dense_weights(const __grid_constant__ WeightsArgs a) {
   extern __shared__ unsigned char smem_raw[];

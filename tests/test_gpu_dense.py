@@ -242,6 +242,60 @@ def test_residual_in_place_streams_and_graph(ctx):
     other.close()
 
 
+def test_a_layer_follows_its_tensors(ctx):
+    """Weights and bias that got other memory between the calls, as a copy of the parameters does it."""
+    import torch
+    from paper_2609_05255_b200 import api
+    x, w, b, _, _, _, _ = make(70, 24, 40, torch.float16, 13)
+    layer = api.DenseLayer(w, b, "relu")
+    y, want = torch.empty((70, 40), device="cuda", dtype=torch.float16), torch.empty((70, 40), device="cuda", dtype=torch.float16)
+    api.gs_dense_forward(ctx, layer, x, y)
+    v, c = (w * 0.5).contiguous(), b + 1
+    api.gs_dense_forward(ctx, api.DenseLayer(v, c, "relu"), x, want)
+    layer.weight.data, layer.bias.data = v.clone(), c.clone()
+    api.gs_dense_forward(ctx, layer, x, y)
+    assert torch.equal(y, want)
+    layer.weight.data = torch.zeros((40, 32), device="cuda", dtype=torch.float16)
+    with pytest.raises(api.GsError):
+        api.gs_dense_forward(ctx, layer, x, y)
+
+
+def test_captured_before_any_other_call():
+    """The first call of a process may be one that is captured: kernels are set up without a word to the stream."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2609_05255_b200 import api
+ctx = api.Context(0)
+h = lambda *s: torch.randn(s, device="cuda").half()
+x, w, dy, z = h(700, 64), h(256, 64), h(700, 256), h(700, 256)
+layer = api.DenseLayer(w, None, "silu")
+outs = lambda: (torch.empty_like(dy), torch.empty_like(x), torch.empty((256, 64), device="cuda"), torch.empty((256,), device="cuda"), torch.empty_like(x))
+ws = torch.empty((api.gs_dense_workspace_bytes(700, 64, 256),), device="cuda", dtype=torch.uint8)
+clip, gws = torch.empty((2,), device="cuda"), torch.empty((api.gs_grad_workspace_bytes(),), device="cuda", dtype=torch.uint8)
+def run(y, dx, dw, db, n):
+    api.gs_dense_forward(ctx, layer, x, y)
+    api.gs_dense_backward(ctx, layer, x, dy, preact=z, dL_dx=dx, dL_dweight=dw, dL_dbias=db, workspace=ws)
+    api.gs_layer_norm_forward(ctx, x, None, None, n)
+    api.gs_clip_grads(ctx, [api.GradTensor(dw, out=dw)], 1.0, clip, gws)
+a, b = outs(), outs()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    run(*a)
+graph.replay()
+run(*b)
+torch.cuda.synchronize()
+assert all(torch.equal(p, q) for p, q in zip(a, b))
+del graph
+ctx.close()
+"""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
+
+
 def test_no_rows(ctx):
     import torch
     from paper_2609_05255_b200 import api
