@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -519,9 +520,23 @@ class AdamTensor:
                             self._more if self.more_grads else None, len(self.more_grads))
 
 
+# The fields of GsAdamTensor in native layout: filling the array by it takes half the time of structs that are copied into it.
+_ADAM_FIELDS = struct.Struct("@5PqiPfffPi0P")
+assert _ADAM_FIELDS.size == C.sizeof(GsAdamTensor)
+
+
+def _adam_array(tensors):
+    arr = (GsAdamTensor * max(1, len(tensors)))()
+    for i, t in enumerate(tensors):
+        _ADAM_FIELDS.pack_into(arr, i * _ADAM_FIELDS.size, _ptr(t.param) or 0, _ptr(t.grad) or 0, _ptr(t.exp_avg) or 0, _ptr(t.exp_avg_sq) or 0,
+                               _ptr(t.half_copy) or 0, t.rows, t.cols, C.addressof(t.lr), t.beta1, t.beta2, t.eps,
+                               C.addressof(t._more) if t.more_grads else 0, len(t.more_grads))
+    return arr
+
+
 def gs_adam_step(ctx: Context, tensors, step: int, stream=None) -> None:
     """Update all `tensors` (AdamTensor objects, at most GS_ADAM_MAX_TENSORS) with one kernel launch."""
-    arr = (GsAdamTensor * max(1, len(tensors)))(*[t.c_struct() for t in tensors])
+    arr = _adam_array(tensors)
     ctx._check(_lib.gs_adam_step(ctx._h, arr, len(tensors), step, _stream_handle(stream)))
 
 
@@ -781,7 +796,7 @@ def gs_clip_grads(ctx: Context, tensors, max_norm: float, clip: torch.Tensor, wo
 
 def gs_adam_step_clipped(ctx: Context, tensors, step: int, clip: torch.Tensor, stream=None) -> None:
     """gs_adam_step with every gradient scaled by clip[1] (from gs_grad_norm); skipped where clip[0] is not finite."""
-    arr = (GsAdamTensor * max(1, len(tensors)))(*[t.c_struct() for t in tensors])
+    arr = _adam_array(tensors)
     ctx._check(_lib.gs_adam_step_clipped(ctx._h, arr, len(tensors), step, _vector(ctx, clip, "clip", 2), _stream_of(ctx, stream)))
 
 # ------------------------------------------------------------------------------------------------
