@@ -748,12 +748,6 @@ GsStatus adam_impl(GsContext *ctx, const GsAdamTensor *tensors, int32_t num_tens
 GsStatus gs_adam_step(GsContext *ctx, const GsAdamTensor *tensors, int32_t num_tensors, int64_t step, void *stream) {
   return adam_impl(ctx, tensors, num_tensors, step, nullptr, stream);
 }
-GsStatus gs_adam_step_clipped(GsContext *ctx, const GsAdamTensor *tensors, int32_t num_tensors, int64_t step, const float *clip, void *stream) {
-  if (!ctx) return GS_ERR_INVALID_ARG;
-  if (!clip || (reinterpret_cast<uintptr_t>(clip) & 7u)) return fail(ctx, GS_ERR_INVALID_ARG, "clip is NULL or misaligned");
-  return adam_impl(ctx, tensors, num_tensors, step, clip, stream);
-}
-
 // ---- layers and clipping ----------------------------------------------------------------------------
 namespace {
 size_t type_bytes(int dtype) { return dtype == GS_TYPE_F32 ? 4 : 2; }
@@ -837,6 +831,13 @@ GsStatus gs_grad_norm(GsContext *ctx, const GsGradTensor *tensors, int32_t num_t
 GsStatus gs_clip_grads(GsContext *ctx, const GsGradTensor *tensors, int32_t num_tensors, float max_norm, float *clip, void *workspace,
                        size_t workspace_bytes, void *stream) {
   return grads_impl(ctx, tensors, num_tensors, true, max_norm, clip, workspace, workspace_bytes, stream);
+}
+
+GsStatus gs_adam_step_clipped(GsContext *ctx, const GsAdamTensor *tensors, int32_t num_tensors, int64_t step, const float *clip, void *stream) {
+  if (!ctx) return GS_ERR_INVALID_ARG;
+  if (!clip || (reinterpret_cast<uintptr_t>(clip) & 7u)) return fail(ctx, GS_ERR_INVALID_ARG, "clip is NULL or misaligned");
+  OnDevice on(ctx->device);
+  return adam_impl(ctx, tensors, num_tensors, step, clip, stream);
 }
 
 GsStatus gs_dense_forward(GsContext *ctx, const GsDenseLayer *layer, int64_t rows, const void *x, int64_t ld_x, const void *residual,

@@ -22,12 +22,12 @@ namespace {
 #include "gs_rows.cuh"
 
 constexpr int kNormThreads = 256;
-constexpr int kNormPartialRows = 592;     // most CTAs of the backward
+constexpr int kNormPartialRows = 960;     // most CTAs of the backward
 
 // CTAs per SM, of as many registers as the elements of a lane need, and no more CTAs than are resident: 1M rows of 256 in bf16
 // forward 189 us with three, 221 with four (spills), 308 with two; backward in fp16 282 with two, 324 with the compiler's choice.
-__host__ __device__ constexpr int fwd_ctas(int elements) { return elements <= 8 ? 4 : elements <= 16 ? 3 : 1; }
-__host__ __device__ constexpr int bwd_ctas(int elements) { return elements <= 8 ? 3 : elements <= 16 ? 2 : 1; }
+__host__ __device__ constexpr int fwd_ctas(int elements) { return elements <= 4 ? 6 : elements <= 8 ? 4 : elements <= 16 ? 3 : 2; }
+__host__ __device__ constexpr int bwd_ctas(int elements) { return elements <= 4 ? 4 : elements <= 8 ? 3 : elements <= 16 ? 2 : 1; }
 
 // How a row is laid over lanes: `lanes` of them with NV vectors of V elements each, vector j of lane l at column (j lanes + l) V.
 // V is a whole 16-byte vector, or 1 where rows are not aligned.
@@ -323,9 +323,11 @@ int fwd_any(const LayerNormArgs &a, int num_sms, cudaStream_t st) {
   const int n = vec ? (a.cols + V - 1) / V : a.cols;
   if (vec) {
     constexpr int few = 16 / V, most = 32 / V;    // vectors of a lane that holds 16 or 32 elements
+    // a row in a warp as long as it fits its registers (100 000 rows of 1024 in bf16 in a CTA's: 192 us), then in as few of a CTA's as it takes
     if (n <= 4) return fwd<T, V, 1, false>(a, lanes_for(n, 1), num_sms, st);
     if (n <= 32 * few) return fwd<T, V, few, false>(a, lanes_for(n, few), num_sms, st);
-    if (n <= kNormThreads) return fwd<T, V, 1, true>(a, kNormThreads, num_sms, st);
+    if (n <= 32 * most) return fwd<T, V, most, false>(a, lanes_for(n, most), num_sms, st);
+    if (n <= kNormThreads * few) return fwd<T, V, few, true>(a, kNormThreads, num_sms, st);
     return fwd<T, V, most, true>(a, kNormThreads, num_sms, st);
   }
   if (n <= 4) return fwd<T, 1, 2, false>(a, lanes_for(n, 2), num_sms, st);
@@ -343,7 +345,8 @@ int bwd_any(const LayerNormArgs &a, int num_sms, cudaStream_t st) {
     constexpr int few = 16 / V, most = 32 / V;    // vectors of a lane that holds 16 or 32 elements
     if (n <= 4) return bwd<T, V, 1, false>(a, lanes_for(n, 1), num_sms, st);
     if (n <= 32 * few) return bwd<T, V, few, false>(a, lanes_for(n, few), num_sms, st);
-    if (n <= kNormThreads) return bwd<T, V, 1, true>(a, kNormThreads, num_sms, st);
+    if (n <= 32 * most) return bwd<T, V, most, false>(a, lanes_for(n, most), num_sms, st);
+    if (n <= kNormThreads * few) return bwd<T, V, few, true>(a, kNormThreads, num_sms, st);
     return bwd<T, V, most, true>(a, kNormThreads, num_sms, st);
   }
   if (n <= 4) return bwd<T, 1, 2, false>(a, lanes_for(n, 2), num_sms, st);
