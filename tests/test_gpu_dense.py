@@ -140,6 +140,16 @@ def test_backward_parts(ctx, want):
     check_backward(ctx, 777, 64, 48, torch.float16, "silu", want=want, seed=10)
 
 
+@pytest.mark.parametrize("rows,cin,cout", [(5, 16384, 16), (3, 16, 16384), (300, 5000, 3001), (9_000_001, 8, 16)])
+def test_the_widest_and_the_longest(ctx, rows, cin, cout):
+    """Weights of hundreds of steps, hundreds of column tiles, and rows whose offsets pass 2^31 bytes when padded."""
+    import torch
+    check_forward(ctx, rows, cin, cout, torch.bfloat16, "silu", residual=True, keep=True, seed=14, pad=240 if rows > 1_000_000 else 0)
+    if rows < 1_000_000:
+        check_backward(ctx, rows, cin, cout, torch.float16, "gelu", seed=15)
+        check_backward(ctx, rows, cin, cout, torch.bfloat16, "relu", seed=16)
+
+
 def test_extreme_preactivations(ctx):
     """act and act' at the ends of the types: 0 or linear, never NaN; a NaN stays in its row."""
     import torch
