@@ -369,8 +369,9 @@ GsStatus gs_dense_forward(GsContext *ctx, const GsDenseLayer *layer, int64_t row
  *   dL_dx = dz W [rows, in_features];  dL_dweight = dz^T x [out_features, in_features] fp32, contiguous;
  *   dL_dbias = sum over rows of dz [out_features] fp32.
  * (dL/dresidual is dL_dy.)  dL_dx, or dL_dweight and dL_dbias, or dL_dbias alone, may be NULL; x may be then without
- * dL_dweight.  preact [rows, out_features] is needed unless the activation is GS_DENSE_NONE.  dz is carried to fp32's accuracy
- * (bf16: 24 bits in dL_dweight and 16 in dL_dx, fp16: 22); in fp16 a dz beyond 65504 makes what it enters not finite, and so does
+ * dL_dweight.  preact [rows, out_features] is needed unless the activation is GS_DENSE_NONE.  With SiLU and GELU dz enters the
+ * products in parts of 16 bits: in bf16 24 bits of it in dL_dweight and 16 in dL_dx, in fp16 22 bits, but none below 2^-36 (gradients
+ * far below 1e-6 want a scale on the loss); with the others it is exact.  In fp16 a dz beyond 65504 makes what it enters not finite, and so does
  * an infinite preact of SiLU or GELU.  The derivative of ReLU at 0 is 0.  Same bits from run to run.  workspace: gs_dense_workspace_bytes(), 16-byte aligned, contents
  * irrelevant; may be NULL without dL_dweight.  GS_ERR_CAPACITY, nothing launched, if it is smaller. */
 size_t gs_dense_workspace_bytes(int64_t rows, int32_t in_features, int32_t out_features);

@@ -20,7 +20,8 @@
 // it: elementwise, so the layout does not matter.  dz is an fp32 product; rounded to 16 bits it would cost dW its fp32 accuracy and dx half
 // again the error of its own rounding.  So for the smooth activations it becomes two or three operands that sum up to
 // it: high, and what the rounding left (which takes the place of preact); three for the weights in bf16, whose two would keep 16 bits.
-// For dW in fp16 what is left is scaled by 2^11 (it would fall below fp16's range) and summed in an accumulator of its own.
+// In fp16 what is left is scaled by 2^11 (it would fall below fp16's range: unscaled, dx lost all but 11 bits of gradients below 2^-13) and
+// summed in an accumulator of its own.
 // Without activation, and with ReLU, dz is dy or 0: exact as it is.
 //
 // Waits are bounded (tma::wait): one that runs out sets *timeout, and the CTA leaves without its results.
@@ -212,6 +213,7 @@ struct RowsArgs {
   int stages, resident;
   int out_slots, keep_slots;                    // tiles of y (where the residual arrives) and preact on their way out: 2 or 4
   int has_keep, has_residual;
+  int accumulators;                             // that tiles take in turn: 2, or 1 where the two parts' fill tensor memory
   uint32_t tmem_cols;
   unsigned long long *timeout;
 };
@@ -231,12 +233,14 @@ template <bool kForward, int kParts> constexpr int kRowsThreads = 32 * (kWarpEpi
 // kForward: B is W [out, in], K-major, and the epilogue has bias, activation, residual and kept pre-activation.  Else B is W
 // [contraction, out], MN-major, A is dz in kParts parts (0: dy as it is).  (The activation is the kernel's: chosen inside, between
 // two unrolled bodies, it kept the values from overlapping.)
+// In fp16 the second part lies 2^11 higher, in the accumulator behind the first one's.
 template <bool kForward, int kAct> constexpr int kRowsParts = kForward || kAct == GS_DENSE_NONE ? 0 : kAct == GS_DENSE_RELU ? 1 : 2;
 template <class T, bool kForward, int kAct, bool kPair>
 __global__ void __launch_bounds__((kRowsThreads<kForward, kRowsParts<kForward, kAct>>), 1) k_dense_rows(const __grid_constant__ RowsArgs a) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char *smem = smem_raw + ((1024u - (tc::smem_addr(smem_raw) & 1023u)) & 1023u);
   constexpr int kParts = kRowsParts<kForward, kAct>;
+  constexpr bool kScale = kParts == 2 && __is_same(T, __half);
   static_assert(!kPair || kParts > 0, "pairs make dz");
   constexpr uint32_t kStageA = kParts ? 2 * kTileBytes : kTileBytes;
   const uint32_t stage_bytes = kStageA + (a.resident ? 0u : a.b_bytes);
@@ -256,12 +260,18 @@ __global__ void __launch_bounds__((kRowsThreads<kForward, kRowsParts<kForward, k
   const int b_cols = a.bn / kCtas;
   const int m_first = worker / a.n_tiles * kCtas + (int)rank, m_step = workers / a.n_tiles * kCtas;
   const int m_end = (a.m_tiles + kCtas - 1) / kCtas * kCtas;      // (a tile behind the last one reads zeros and writes nothing)
-  const uint32_t acc_cols = (uint32_t)(a.bn + 63) & ~63u;
+  const uint32_t acc_cols = (uint32_t)(a.bn + 63) & ~63u, acc_stride = kScale ? 2 * acc_cols : acc_cols;
+  // the accumulator of this CTA's tile-th tile, and its pass over it
+  auto acc_of = [&](uint32_t tile) { return kScale && a.accumulators == 1 ? 0u : tile & 1u; };
+  auto acc_use = [&](uint32_t tile) { return kScale && a.accumulators == 1 ? tile : tile >> 1; };
   const int chunks = (min(a.bn, a.out_cols - n0) + 63) / 64;
+  // One accumulator and one chunk: the groups that take tiles out have one every other pass, but a parity tells only neighbouring passes
+  // apart, so a group follows the passes of the other, too, and the accumulator is empty when it has seen them.
+  const bool follow = kScale && a.accumulators == 1 && chunks == 1;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < a.stages; ++s) { tma::init(bar(bars.full[s]), 1); tma::init(bar(bars.ready[s]), kCtas * kTransformThreads / 32); tma::init(bar(bars.empty[s]), 1); }
-    for (int i = 0; i < 2; ++i) { tma::init(bar(bars.acc_full[i]), 1); tma::init(bar(bars.acc_empty[i]), kCtas * chunks * kGroup); }
+    for (int i = 0; i < 2; ++i) { tma::init(bar(bars.acc_full[i]), 1); tma::init(bar(bars.acc_empty[i]), kCtas * (chunks * kGroup + (follow ? 1 : 0))); }
     for (int i = 0; i < 4; ++i) { tma::init(bar(bars.res_full[i]), 1); tma::init(bar(bars.res_empty[i]), 1); }
     tma::init(bar(bars.weights), 1); tma::init(bar(bars.weights_both), 1); tma::init(bar(bars.drained), 1);
     bars.dead = 0u;
@@ -332,9 +342,9 @@ __global__ void __launch_bounds__((kRowsThreads<kForward, kRowsParts<kForward, k
       Ring at;
       bool ok = !a.resident || (tma::wait(bar(bars.weights), 0u, dead) && (!kPair || tma::wait<kPair>(bar(bars.weights_both), 0u, dead)));
       for (int m = m_first; ok && m < m_end; m += m_step, ++tile) {
-        const uint32_t buf = tile & 1u;
-        if (!(ok = tma::wait<kPair>(bar(bars.acc_empty[buf]), (tile >> 1 & 1u) ^ 1u, dead))) break;
-        const uint32_t d = tmem + buf * acc_cols;
+        const uint32_t buf = acc_of(tile);
+        if (!(ok = tma::wait<kPair>(bar(bars.acc_empty[buf]), (acc_use(tile) & 1u) ^ 1u, dead))) break;
+        const uint32_t d = tmem + buf * acc_stride;
         for (int kb = 0; kb < a.k_blocks; ++kb, at.next(a.stages)) {
           const uint64_t da = a_desc + at.s * stage16, db = b_desc + (a.resident ? kb * b16 : at.s * stage16);
           if (!(ok = tma::wait<kPair>(ready0 + at.s * 8, at.parity, dead))) break;
@@ -344,7 +354,7 @@ __global__ void __launch_bounds__((kRowsThreads<kForward, kRowsParts<kForward, k
           for (int p = 0; p < (kParts == 2 ? 2 : 1); ++p)
 #pragma unroll
             for (int ks = 0; ks < 4; ++ks)
-              if (ks < steps) mma(d, da + p * (kTileBytes >> 4) + ks * 2, db + ks * kNextB, p || ks ? 1u : (uint32_t)kb, desc);
+              if (ks < steps) mma(kScale && p ? d + acc_cols : d, da + p * (kTileBytes >> 4) + ks * 2, db + ks * kNextB, (p && !kScale) || ks ? 1u : (uint32_t)kb, desc);
           commit(empty0 + at.s * 8);
         }
         if (ok) commit(bar(bars.acc_full[buf]));
@@ -392,10 +402,15 @@ __global__ void __launch_bounds__((kRowsThreads<kForward, kRowsParts<kForward, k
     Ring at;
     bool ok = true;
     for (int m = m_first; ok && m < m_end; m += m_step, ++tile) {
-      const uint32_t buf = tile & 1u;
+      const uint32_t buf = acc_of(tile);
       for (int c = 0; c < chunks; ++c, at.next(a.out_slots)) {
         const uint32_t s = at.s;
-        if ((int)(s & 1u) != group) continue;
+        if ((int)(s & 1u) != group) {
+          if (follow && tid == 0 && tma::wait(bar(bars.acc_full[buf]), acc_use(tile) & 1u, dead)) {
+            if (kPair) pair::arrive_first(bar(bars.acc_empty[buf])); else tma::arrive(bar(bars.acc_empty[buf]));
+          }
+          continue;
+        }
         if (tid == 0) {
           if (kForward && a.has_residual) {                        // the slot before is free for the residual of a chunk to come
             tma::stores_read<0>();
@@ -406,7 +421,7 @@ __global__ void __launch_bounds__((kRowsThreads<kForward, kRowsParts<kForward, k
           } else {
             tma::stores_read<0>();
           }
-          bool all = tma::wait(bar(bars.acc_full[buf]), tile >> 1 & 1u, dead);
+          bool all = tma::wait(bar(bars.acc_full[buf]), acc_use(tile) & 1u, dead);
           if (kForward && a.has_residual) all = all && tma::wait(bar(bars.res_full[s]), at.parity, dead);
           bars.ok[group] = all ? 1u : 0u;
         }
@@ -419,7 +434,17 @@ __global__ void __launch_bounds__((kRowsThreads<kForward, kRowsParts<kForward, k
         for (int half = 0; half < (kGroup == 8 ? 1 : 2); ++half) {
           const int h = kGroup == 8 ? tid >> 7 : half;
           float2 v[16];
-          load32(tmem + buf * acc_cols + c * 64 + h * 32 + ((uint32_t)(tid & 96) << 16), &v[0].x);
+          const uint32_t from = tmem + buf * acc_stride + c * 64 + h * 32 + ((uint32_t)(tid & 96) << 16);
+          load32(from, &v[0].x);
+          if constexpr (kScale) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              float2 l[8];
+              tc::load16(from + acc_cols + q * 16, &l[0].x);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[q * 8 + i] = fma2(l[i], both(1.f / 2048.f), v[q * 8 + i]);
+            }
+          }
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const uint32_t in = (uint32_t)((h * 4 + q) ^ (row & 7)) * 16u;
@@ -479,7 +504,7 @@ __global__ void __launch_bounds__((kRowsThreads<kForward, kRowsParts<kForward, k
 #pragma unroll
         for (int u = 0; u < kChunks; ++u) {
           unsigned char *p = A + (u * kTransformThreads + t) * 16;
-          transform_chunk<T, kAct, kParts, false, false>(p, p + kTileBytes, nullptr, dy[u], z[u], nullptr);
+          transform_chunk<T, kAct, kParts, kScale, false>(p, p + kTileBytes, nullptr, dy[u], z[u], nullptr);
         }
         tc::fence_generic_writes();
         __syncwarp();
@@ -832,8 +857,8 @@ bool shape_rows(RowsArgs &a, bool forward, bool transform, int bn, int ctas, boo
   }
   return false;
 }
-// The number of CTAs that share a tile's weights, or 0.
-int plan_rows(RowsArgs &a, bool forward, bool transform, int num_sms, uint32_t &smem, int &grid) {
+// The number of CTAs that share a tile's weights, or 0.  scaled: the second part of dz has accumulators of its own.
+int plan_rows(RowsArgs &a, bool forward, bool transform, bool scaled, int num_sms, uint32_t &smem, int &grid) {
   // Wide tiles read the rows once; narrower ones where there are fewer tiles than SMs.  Results leave in boxes of 64 columns, so tiles
   // beside one another are a multiple of that.
   int bn = a.out_cols <= 256 ? (a.out_cols + 15) / 16 * 16 : 256, ctas = 1;
@@ -842,9 +867,12 @@ int plan_rows(RowsArgs &a, bool forward, bool transform, int num_sms, uint32_t &
   const int narrow = bn > 128 ? 128 : bn;
   // Where dz is made, tiles of more than 128 columns by pairs of CTAs, each with half of the weights, which leaves room for three or
   // four steps of dy and preact instead of two: dx of 1M rows of 256 to 256 in bf16 with SiLU 295 us instead of 353, with ReLU 237
-  // instead of 287.  Without dz the steps are small and the first CTA's wait for both costs more than it brings: 181 instead of
+  // instead of 287.  Four steps where the second part has its own accumulator and the next tile's products wait for this one's to leave: fp16
+  // 335 us instead of 357 with three (308 with both parts in one accumulator, without the bits that fp16 then loses).  Without dz the steps are small and the first CTA's wait for both costs more than it brings: 181 instead of
   // 164, forward with residual 350 instead of 313, 20 011 rows of 1024 to 1024 55 instead of 50.
-  if (transform && bn > 128 && a.m_tiles >= 2 && shape_rows(a, forward, transform, 256, 2, true, 3, smem)) ctas = 2;
+  if (transform && bn > 128 && a.m_tiles >= 2 &&
+      ((scaled && shape_rows(a, forward, transform, 256, 2, true, 4, smem)) || shape_rows(a, forward, transform, 256, 2, true, 3, smem)))
+    ctas = 2;
   // Else resident weights, up to six steps of a narrower tile if need be (forward, 300 000 rows of 256 to 256 with residual and kept
   // pre-activation 103 us instead of 153; 100 000 of 320 to 512 85 instead of 110), beyond that weights that come with every step
   // rather than two looks at the rows (100 000 of 512 to 512 65 instead of 83).
@@ -852,7 +880,9 @@ int plan_rows(RowsArgs &a, bool forward, bool transform, int num_sms, uint32_t &
                      shape_rows(a, forward, transform, bn, 1, false, 3, smem) || shape_rows(a, forward, transform, narrow, 1, true, 3, smem) ||
                      shape_rows(a, forward, transform, narrow, 1, false, 2, smem)))
     return 0;
-  a.tmem_cols = tmem_columns(2u * (((uint32_t)a.bn + 63u) & ~63u));
+  const uint32_t acc = (((uint32_t)a.bn + 63u) & ~63u) * (scaled ? 2u : 1u);
+  a.accumulators = 2u * acc <= 512u ? 2 : 1;
+  a.tmem_cols = tmem_columns((uint32_t)a.accumulators * acc);
   const int tiles = ceil_div(a.m_tiles, ctas);
   int groups = num_sms / ctas / a.n_tiles;
   if (groups < 1) groups = 1;
@@ -911,7 +941,7 @@ int fwd(const DenseArgs &d, int num_sms, cudaStream_t st) {
   a.has_keep = d.preact != nullptr; a.has_residual = d.residual != nullptr; a.timeout = d.timeout;
   uint32_t smem;
   int grid;
-  if (!plan_rows(a, true, false, num_sms, smem, grid)) return -1;
+  if (!plan_rows(a, true, false, false, num_sms, smem, grid)) return -1;
   if (!tma::make_map(&a.a, d.dtype, d.x, d.rows, d.in, d.ld_x, kRows) || !tma::make_map(&a.b, d.dtype, d.w, d.out, d.in, d.ld_w, a.bn) ||
       (d.out >= 8 && !tma::make_map(&a.out, d.dtype, d.y, d.rows, d.out & ~7, d.ld_y, kRows)) ||
       (d.out >= 8 && a.has_keep && !tma::make_map(&a.keep, d.dtype, d.preact, d.rows, d.out & ~7, d.ld_preact, kRows)) ||
@@ -973,7 +1003,7 @@ int bwd(const DenseArgs &d, int num_sms, cudaStream_t st) {
     a.has_keep = a.has_residual = 0; a.timeout = d.timeout;
     uint32_t smem;
     int grid;
-    const int ctas = plan_rows(a, false, !plain, num_sms, smem, grid);
+    const int ctas = plan_rows(a, false, !plain, d.dtype == GS_TYPE_F16 && (d.act == GS_DENSE_SILU || d.act == GS_DENSE_GELU), num_sms, smem, grid);
     if (!ctas) return -1;
     if (!tma::make_map(&a.a, d.dtype, d.dy, d.rows, d.out, d.ld_dy, kRows) || !tma::make_map(&a.b, d.dtype, d.w, d.out, d.in, d.ld_w, kStep) ||
         (d.in >= 8 && !tma::make_map(&a.out, d.dtype, d.dx, d.rows, d.in & ~7, d.ld_dx, kRows)) ||
