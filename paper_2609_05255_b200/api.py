@@ -619,7 +619,7 @@ def _workspace(ctx: Context, t: Optional[torch.Tensor]):
 class DenseLayer:
     """Weights of a dense layer: weight [out, in] float16 or bfloat16 (rows a multiple of eight elements apart), bias [out]
     float32 or None, activation "none", "relu", "silu" or "gelu" (or its GS_DENSE_ number).  Marshalling only: it holds the tensors, whose
-    values may change between calls."""
+    values, memory and type may change between calls (and the bias may come and go), but not their sizes."""
 
     def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, activation="none"):
         if weight.dim() != 2 or weight.dtype not in _TYPES or (weight.stride(1) != 1 and weight.shape[1] > 1) or not weight.is_cuda:
@@ -653,13 +653,15 @@ def gs_dense_workspace_bytes(rows: int, in_features: int, out_features: int) -> 
 
 
 def _layer(ctx: Context, layer: DenseLayer) -> GsDenseLayer:
-    """The layer's struct with the addresses that its tensors have now."""
+    """The layer's struct with the addresses, the type and the row stride that its tensors have now."""
     s, w = layer._struct, layer.weight
-    if w.device != ctx.device or w.shape != (s.out_features, s.in_features):
-        _invalid(f"the layer's weight is {list(w.shape)} on {w.device}, the layer made for [{s.out_features}, {s.in_features}], the context on {ctx.device}")
-    s.weight, s.ld_weight = w.data_ptr(), w.stride(0) if s.out_features > 1 else (s.in_features + 7) // 8 * 8
-    if layer.bias is not None:
-        s.bias = _vector(ctx, layer.bias, "bias", s.out_features)
+    if w.device != ctx.device or w.shape != (s.out_features, s.in_features) or w.dtype not in _TYPES:
+        _invalid(f"the layer's weight is {w.dtype} {list(w.shape)} on {w.device}, the layer made for [{s.out_features}, {s.in_features}], the context on {ctx.device}")
+    ld, one = w.stride()
+    if one != 1 and s.in_features > 1:
+        _invalid("the layer's weight: the values of a row must be contiguous")
+    s.weight, s.ld_weight, s.dtype = w.data_ptr(), ld if s.out_features > 1 else (s.in_features + 7) // 8 * 8, _TYPES[w.dtype]
+    s.bias = _vector(ctx, layer.bias, "bias", s.out_features)
     return s
 
 
