@@ -224,9 +224,10 @@ GsStatus gs_preprocess_async(GsContext *ctx, const GsScene *scene, const GsCamer
  * on a stream that is being captured. */
 GsStatus gs_async_pairs(GsContext *ctx, int64_t *num_pairs_host, void *stream);
 /* Waits for `stream`, then returns GS_ERR_CAPACITY if any device-counted view on this context
- * overflowed its pair_capacity since the last call (and clears the flag), GS_ERR_INTERNAL if a kernel
- * gave up a bounded wait on one of its own bulk copies (never expected; the waits exist so that a
- * kernel cannot hang), else GS_OK. */
+ * overflowed its pair_capacity since the last call (and clears the flag), GS_ERR_INTERNAL if a kernel of the
+ * context (appearance, dense layers) gave up a bounded wait for its own copies, products or the CTA it is paired
+ * with (never expected; the waits exist so that a kernel cannot hang), else GS_OK.  Results of the calls since the last
+ * gs_async_status are then incomplete. */
 GsStatus gs_async_status(GsContext *ctx, void *stream);
 
 /* Tile assignment, ordering and blending (Sec. 3.1, blend kernel).  Orders the visible
@@ -361,7 +362,9 @@ typedef struct {
 /* y = act(x W^T + bias) + residual.  x [rows, in_features], y and residual [rows, out_features] in the layer's type, 16-byte
  * aligned with ld a multiple of 8 (the columns may be any number).  residual may be NULL, or y itself.  preact (may be
  * NULL) receives x W^T + bias, rounded to the layer's type: what gs_dense_backward wants of a layer with an
- * activation.  Sums, bias, activation and residual are taken in fp32, y is rounded once. */
+ * activation.  Sums, bias, activation and residual are taken in fp32, y is rounded once.
+ * Dense layers, forward and backward, return before the GPU is done: that a bounded wait of theirs ran out (never expected),
+ * which leaves y, preact or the gradients incomplete, is what gs_async_status tells. */
 GsStatus gs_dense_forward(GsContext *ctx, const GsDenseLayer *layer, int64_t rows, const void *x, int64_t ld_x,
                           const void *residual, int64_t ld_residual, void *y, int64_t ld_y, void *preact, int64_t ld_preact,
                           void *stream);

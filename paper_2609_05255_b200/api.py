@@ -394,7 +394,8 @@ def gs_async_pairs(ctx: Context, stream=None) -> int:
 
 
 def gs_async_status(ctx: Context, stream=None) -> None:
-    """Wait for the stream; raise GsError(GS_ERR_CAPACITY) if a device-counted view overflowed its capacity."""
+    """Wait for the stream; raise GsError: GS_ERR_CAPACITY if a device-counted view overflowed its capacity, GS_ERR_INTERNAL if a
+    bounded wait of a kernel ran out (appearance, dense layers; never expected), which leaves results incomplete."""
     ctx._check(_lib.gs_async_status(ctx._h, _stream_handle(stream)))
 
 

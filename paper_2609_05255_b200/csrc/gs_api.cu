@@ -391,7 +391,7 @@ GsStatus gs_async_status(GsContext *ctx, void *stream) {
   if ((st = check_cuda(ctx, cudaMemsetAsync(ctx->d_counter + 2, 0, 2 * sizeof(unsigned long long), s), "status reset")) != GS_OK) return st;
   if ((st = check_cuda(ctx, cudaStreamSynchronize(s), "status")) != GS_OK) return st;
   if (ctx->h_counter[3] != 0)
-    return fail(ctx, GS_ERR_INTERNAL, "a bounded wait on a bulk copy ran out in an appearance kernel: its results are incomplete");
+    return fail(ctx, GS_ERR_INTERNAL, "a bounded wait ran out in an appearance or dense-layer kernel: its results are incomplete");
   if (ctx->h_counter[2] != 0)
     return fail(ctx, GS_ERR_CAPACITY, "a device-counted gs_render_forward had more instances than pair_capacity: that view's lists were cut off");
   return GS_OK;
