@@ -211,17 +211,19 @@ __global__ void __launch_bounds__(kNormThreads, bwd_ctas(V * NV)) k_layer_norm_b
     float2 s = make_float2(0.f, 0.f), t = s;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      // columns behind the row's end have dy = 0: nothing comes of them whatever h is there
-      h[i] = mul2(add2(h[i], minus), r);
+      // the sum of g h as rstd times that of g (x - mean): columns behind the row's end have g = 0 and x = 0, so their terms are 0 (their h
+      // would be -mean rstd, which may be infinite)
+      const float2 d = add2(h[i], minus);
+      h[i] = mul2(d, r);
       if (kParams) {
         sum_g[i] = fma2(g[i], h[i], sum_g[i]);
         sum_b[i] = add2(sum_b[i], g[i]);
       }
       g[i] = mul2(g[i], gamma[i]);
       s = add2(s, g[i]);
-      t = fma2(g[i], h[i], t);
+      t = fma2(g[i], d, t);
     }
-    const float2 sums = group_sum2<kBlock>(make_float2(s.x + s.y, t.x + t.y), lanes, shared);
+    const float2 sums = group_sum2<kBlock>(make_float2(s.x + s.y, (t.x + t.y) * r.x), lanes, shared);
     if (row < a.rows && a.dx) {
       const float2 avg_g = both(-sums.x * inv), avg_gh = both(-sums.y * inv);
 #pragma unroll
