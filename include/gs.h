@@ -338,7 +338,7 @@ GsStatus gs_adam_step(GsContext *ctx, const GsAdamTensor *tensors, int32_t num_t
  * The paper has no counterpart.
  *
  * Rows of activations lie `ld` elements apart (ld >= columns); columns behind the last one are neither read nor written.  No
- * two arguments of a call overlap, but where it is said.  rows may be 0 and stays below 2^31. */
+ * two arguments of a call overlap, but where it is said, and then they have the same ld.  rows may be 0 and stays below 2^31. */
 typedef enum { GS_TYPE_F32 = 0, GS_TYPE_F16 = 1, GS_TYPE_BF16 = 2 } GsType;
 typedef enum {
   GS_DENSE_NONE = 0,

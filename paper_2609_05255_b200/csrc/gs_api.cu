@@ -778,6 +778,8 @@ GsStatus dense_ok(GsContext *ctx, const GsDenseLayer *l, int64_t rows) {
   if (l->bias && (reinterpret_cast<uintptr_t>(l->bias) & 3u)) return fail(ctx, GS_ERR_INVALID_ARG, "bias is misaligned");
   return GS_OK;
 }
+// An output in the place of an input has the input's rows: other strides would make rows overlap others.
+bool rows_shifted(const void *out, int64_t ld_out, const void *in, int64_t ld_in, int64_t rows) { return out == in && rows > 1 && ld_out != ld_in; }
 // A matrix that moves by TMA.
 bool matrix_bad(const void *p, int64_t ld, int32_t cols) { return bad_ptr(p) || ld < cols || (ld & 7) || ld >= ((int64_t)1 << 38); }
 
@@ -848,6 +850,7 @@ GsStatus gs_dense_forward(GsContext *ctx, const GsDenseLayer *layer, int64_t row
   if (matrix_bad(x, ld_x, layer->in_features) || matrix_bad(y, ld_y, layer->out_features) ||
       (residual && matrix_bad(residual, ld_residual, layer->out_features)) || (preact && matrix_bad(preact, ld_preact, layer->out_features)))
     return fail(ctx, GS_ERR_INVALID_ARG, "a matrix is NULL or misaligned, or its ld is no multiple of 8 or shorter than a row");
+  if (residual && rows_shifted(y, ld_y, residual, ld_residual, rows)) return fail(ctx, GS_ERR_INVALID_ARG, "y in the residual's place has another ld");
   DenseArgs a = {};
   a.rows = rows; a.in = layer->in_features; a.out = layer->out_features; a.dtype = layer->dtype; a.act = layer->activation;
   a.x = x; a.w = layer->weight; a.residual = residual; a.ld_x = ld_x; a.ld_w = layer->ld_weight; a.ld_residual = ld_residual;
@@ -929,6 +932,7 @@ GsStatus gs_layer_norm_forward(GsContext *ctx, int32_t dtype, int64_t rows, int3
   if (!(eps > 0.f)) return fail(ctx, GS_ERR_INVALID_ARG, "eps must be above 0");
   if (rows == 0) return GS_OK;
   if (rows_bad(x, ld_x, cols, dtype) || rows_bad(y, ld_y, cols, dtype)) return fail(ctx, GS_ERR_INVALID_ARG, "x or y is NULL or misaligned, or its ld shorter than a row");
+  if (rows_shifted(y, ld_y, x, ld_x, rows)) return fail(ctx, GS_ERR_INVALID_ARG, "y in the place of x has another ld");
   if (floats_bad(gamma) || floats_bad(beta) || floats_bad(mean) || floats_bad(rstd)) return fail(ctx, GS_ERR_INVALID_ARG, "a vector is misaligned");
   LayerNormArgs a = {};
   a.rows = rows; a.cols = cols; a.dtype = dtype; a.x = x; a.y = y; a.ld_x = ld_x; a.ld_out = ld_y; a.gamma = gamma; a.beta = beta;
@@ -964,6 +968,8 @@ GsStatus gs_layer_norm_backward(GsContext *ctx, int32_t dtype, int64_t rows, int
   }
   if (rows_bad(dL_dy, ld_dy, cols, dtype) || rows_bad(x, ld_x, cols, dtype) || (dL_dx && rows_bad(dL_dx, ld_dx, cols, dtype)) || !mean || !rstd)
     return fail(ctx, GS_ERR_INVALID_ARG, "dL_dy, x, dL_dx, mean or rstd is NULL or misaligned, or an ld shorter than a row");
+  if (dL_dx && (rows_shifted(dL_dx, ld_dx, dL_dy, ld_dy, rows) || rows_shifted(dL_dx, ld_dx, x, ld_x, rows)))
+    return fail(ctx, GS_ERR_INVALID_ARG, "dL_dx in the place of dL_dy or x has another ld");
   if ((dL_dgamma || dL_dbeta) && bad_ptr(workspace)) return fail(ctx, GS_ERR_INVALID_ARG, "workspace is NULL or misaligned");
   if ((dL_dgamma || dL_dbeta) && workspace_bytes < gs_layer_norm_workspace_bytes(rows, cols))
     return fail(ctx, GS_ERR_CAPACITY, "workspace smaller than gs_layer_norm_workspace_bytes()");
