@@ -352,7 +352,7 @@ enum { GS_DENSE_MAX_FEATURES = 16384, GS_LAYER_NORM_MAX_COLS = 8192, GS_GRAD_MAX
  * (out, in), in fp16 or bf16; bias [out_features] fp32, or NULL. */
 typedef struct {
   const void *weight;
-  int64_t ld_weight;           /* elements from row to row; a multiple of 8                          */
+  int64_t ld_weight;           /* elements from row to row; a multiple of 8, below 2^38              */
   const float *bias;
   int32_t in_features, out_features;   /* 1 .. GS_DENSE_MAX_FEATURES                                 */
   int32_t dtype;               /* GS_TYPE_F16 or GS_TYPE_BF16: of weight and of all activations      */
@@ -360,7 +360,7 @@ typedef struct {
 } GsDenseLayer;
 
 /* y = act(x W^T + bias) + residual.  x [rows, in_features], y and residual [rows, out_features] in the layer's type, 16-byte
- * aligned with ld a multiple of 8 (the columns may be any number).  residual may be NULL, or y itself.  preact (may be
+ * aligned with ld a multiple of 8 below 2^38 (the columns may be any number).  residual may be NULL, or y itself.  preact (may be
  * NULL) receives x W^T + bias, rounded to the layer's type: what gs_dense_backward wants of a layer with an
  * activation.  Sums, bias, activation and residual are taken in fp32, y is rounded once.
  * Dense layers, forward and backward, return before the GPU is done: that a bounded wait of theirs ran out (never expected),

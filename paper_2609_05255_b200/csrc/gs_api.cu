@@ -773,8 +773,8 @@ GsStatus dense_ok(GsContext *ctx, const GsDenseLayer *l, int64_t rows) {
     return fail(ctx, GS_ERR_INVALID_ARG, "in_features and out_features must be 1..16384");
   if (rows < 0) return fail(ctx, GS_ERR_INVALID_ARG, "rows < 0");
   if (rows >= ((int64_t)1 << 31)) return fail(ctx, GS_ERR_CAPACITY, "rows must stay below 2^31");
-  if (bad_ptr(l->weight) || l->ld_weight < l->in_features || (l->ld_weight & 7))
-    return fail(ctx, GS_ERR_INVALID_ARG, "weight is NULL or misaligned, or ld_weight is no multiple of 8 or shorter than a row");
+  if (bad_ptr(l->weight) || l->ld_weight < l->in_features || (l->ld_weight & 7) || l->ld_weight >= ((int64_t)1 << 38))
+    return fail(ctx, GS_ERR_INVALID_ARG, "weight is NULL or misaligned, or ld_weight is no multiple of 8, shorter than a row or 2^38 or more");
   if (l->bias && (reinterpret_cast<uintptr_t>(l->bias) & 3u)) return fail(ctx, GS_ERR_INVALID_ARG, "bias is misaligned");
   return GS_OK;
 }
@@ -862,7 +862,7 @@ GsStatus gs_dense_forward(GsContext *ctx, const GsDenseLayer *layer, int64_t row
   {
     StageTimer t(ctx, GS_STAGE_DENSE, s);
     launches = launch_dense_fwd(a, ctx->num_sms, s);
-    t.done(launches);
+    t.done(launches > 0 ? launches : 0);
   }
   if (launches < 0) return fail(ctx, GS_ERR_INTERNAL, "the driver refused a tensor map");
   return check_cuda(ctx, cudaGetLastError(), "dense forward launch");
@@ -907,7 +907,7 @@ GsStatus gs_dense_backward(GsContext *ctx, const GsDenseLayer *layer, int64_t ro
   {
     StageTimer t(ctx, GS_STAGE_DENSE, s);
     launches = launch_dense_bwd(a, ctx->num_sms, s);
-    t.done(launches);
+    t.done(launches > 0 ? launches : 0);
   }
   if (launches < 0) return fail(ctx, GS_ERR_INTERNAL, "the driver refused a tensor map");
   return check_cuda(ctx, cudaGetLastError(), "dense backward launch");

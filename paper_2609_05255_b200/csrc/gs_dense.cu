@@ -992,47 +992,52 @@ void run_weights(WeightsArgs &a, cudaStream_t st) {
   run_weights_as<T, kAct, false>(a, st);
 }
 
+// Every tensor map is made before the first launch: a call whose map the driver refuses launches nothing.
 template <class T>
 int bwd(const DenseArgs &d, int num_sms, cudaStream_t st) {
   const bool plain = d.act == GS_DENSE_NONE;
   int launches = 0;
+  RowsArgs a;
+  uint32_t smem = 0;
+  int grid = 0, ctas = 0;
   if (d.dx) {
-    RowsArgs a;
     a.bias = nullptr; a.out_cols = d.in; a.k = d.out; a.k_blocks = ceil_div(d.out, kStep); a.m_tiles = ceil_div(d.rows, kRows);
     a.rows = (int)d.rows; a.out_rows = d.dx; a.ld_out = d.ld_dx; a.keep_rows = nullptr; a.ld_keep = 0;
     a.has_keep = a.has_residual = 0; a.timeout = d.timeout;
-    uint32_t smem;
-    int grid;
-    const int ctas = plan_rows(a, false, !plain, d.dtype == GS_TYPE_F16 && (d.act == GS_DENSE_SILU || d.act == GS_DENSE_GELU), num_sms, smem, grid);
+    ctas = plan_rows(a, false, !plain, d.dtype == GS_TYPE_F16 && (d.act == GS_DENSE_SILU || d.act == GS_DENSE_GELU), num_sms, smem, grid);
     if (!ctas) return -1;
     if (!tma::make_map(&a.a, d.dtype, d.dy, d.rows, d.out, d.ld_dy, kRows) || !tma::make_map(&a.b, d.dtype, d.w, d.out, d.in, d.ld_w, kStep) ||
         (d.in >= 8 && !tma::make_map(&a.out, d.dtype, d.dx, d.rows, d.in & ~7, d.ld_dx, kRows)) ||
         (!plain && !tma::make_map(&a.z, d.dtype, d.preact_in, d.rows, d.out, d.ld_preact, kRows)))
       return -1;
+  }
+  WeightsArgs w;
+  if (d.dw) {
+    const WeightsPlan p = plan_weights(d.rows, d.in, d.out, num_sms < kSplitSms ? num_sms : kSplitSms);
+    w.n = d.out; w.k = d.in; w.n_tiles = p.n_tiles; w.k_tiles = p.k_tiles; w.splits = p.splits; w.bk = p.bk; w.ld = p.ld;
+    w.row_blocks = ceil_div(d.rows, kWStep); w.want_db = d.db != nullptr; w.timeout = d.timeout;
+    w.partials = d.partials;
+    w.db_partials = d.partials + (size_t)p.splits * d.out * p.ld;
+    if (!tma::make_map(&w.dy, d.dtype, d.dy, d.rows, d.out, d.ld_dy, kWStep) || !tma::make_map(&w.x, d.dtype, d.x, d.rows, d.in, d.ld_x, kWStep) ||
+        (!plain && !tma::make_map(&w.z, d.dtype, d.preact_in, d.rows, d.out, d.ld_preact, kWStep)))
+      return -1;
+  }
+  if (d.dx) {
     if (ctas == 2) run_pairs<T>(d.act, a, smem, grid, st);
     else run_rows<T, false>(d.act, a, smem, grid, st);
     ++launches;
   }
   if (d.dw) {
-    const WeightsPlan p = plan_weights(d.rows, d.in, d.out, num_sms < kSplitSms ? num_sms : kSplitSms);
-    WeightsArgs a;
-    a.n = d.out; a.k = d.in; a.n_tiles = p.n_tiles; a.k_tiles = p.k_tiles; a.splits = p.splits; a.bk = p.bk; a.ld = p.ld;
-    a.row_blocks = ceil_div(d.rows, kWStep); a.want_db = d.db != nullptr; a.timeout = d.timeout;
-    a.partials = d.partials;
-    a.db_partials = d.partials + (size_t)p.splits * d.out * p.ld;
-    if (!tma::make_map(&a.dy, d.dtype, d.dy, d.rows, d.out, d.ld_dy, kWStep) || !tma::make_map(&a.x, d.dtype, d.x, d.rows, d.in, d.ld_x, kWStep) ||
-        (!plain && !tma::make_map(&a.z, d.dtype, d.preact_in, d.rows, d.out, d.ld_preact, kWStep)))
-      return -1;
-    if (d.act == GS_DENSE_NONE) run_weights<T, GS_DENSE_NONE>(a, st);
-    else if (d.act == GS_DENSE_RELU) run_weights<T, GS_DENSE_RELU>(a, st);
-    else if (d.act == GS_DENSE_SILU) run_weights<T, GS_DENSE_SILU>(a, st);
-    else run_weights<T, GS_DENSE_GELU>(a, st);
+    if (d.act == GS_DENSE_NONE) run_weights<T, GS_DENSE_NONE>(w, st);
+    else if (d.act == GS_DENSE_RELU) run_weights<T, GS_DENSE_RELU>(w, st);
+    else if (d.act == GS_DENSE_SILU) run_weights<T, GS_DENSE_SILU>(w, st);
+    else run_weights<T, GS_DENSE_GELU>(w, st);
     auto sum = [&](auto kernel, int values) {
-      const int blocks = ceil_div((int64_t)d.out * p.ld, values);
-      launch_chained(kernel, blocks + (d.db ? ceil_div(d.out, values) : 0), 512, 0, st, (const float *)a.partials, (const float *)a.db_partials, p.splits, d.out, d.in,
-                     p.ld, blocks, d.dw, d.db);
+      const int blocks = ceil_div((int64_t)d.out * w.ld, values);
+      launch_chained(kernel, blocks + (d.db ? ceil_div(d.out, values) : 0), 512, 0, st, (const float *)w.partials, (const float *)w.db_partials, w.splits, d.out, d.in,
+                     w.ld, blocks, d.dw, d.db);
     };
-    if (p.splits >= 16) sum(k_dense_sums<16>, 128);
+    if (w.splits >= 16) sum(k_dense_sums<16>, 128);
     else sum(k_dense_sums<1>, 2048);
     launches += 2;
   }
