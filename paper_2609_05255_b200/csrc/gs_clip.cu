@@ -32,8 +32,8 @@ struct GradEntry {
   uint32_t chunk_start;                   // chunks of the tensors before
   uint16_t more_start;                    // its further buffers in the table of pointers
   uint8_t num_more, dtype;
-  uint32_t head;                          // elements before the first 16-byte boundary; all of them (count) where the buffers'
-  uint32_t pad;                           // boundaries differ: element by element then
+  uint32_t head;                          // elements before the first 16-byte boundary; 2^32 - 1 where the buffers' boundaries differ:
+                                          // element by element then
 };
 // The tables travel as kernel parameters: nothing to allocate or copy, and a captured launch keeps its own.
 template <int kTensors, int kMore>
@@ -239,7 +239,7 @@ int run(const GsGradTensor *tensors, int num_tensors, bool scale, float max_norm
     const GsGradTensor &s = tensors[i];
     if (s.count == 0) continue;
     GradEntry &d = a.t[a.num_tensors++];
-    d.grad = s.grad; d.out = scale ? s.out : nullptr; d.count = (uint64_t)s.count; d.pad = 0;
+    d.grad = s.grad; d.out = scale ? s.out : nullptr; d.count = (uint64_t)s.count;
     d.chunk_start = a.chunks; d.more_start = (uint16_t)more; d.num_more = (uint8_t)s.num_more_grads; d.dtype = (uint8_t)s.dtype;
     const uintptr_t at = reinterpret_cast<uintptr_t>(s.grad) & 15u;
     bool same = !scale || (reinterpret_cast<uintptr_t>(s.out) & 15u) == at;
