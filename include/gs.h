@@ -403,7 +403,8 @@ GsStatus gs_layer_norm_backward(GsContext *ctx, int32_t dtype, int64_t rows, int
 /* A gradient for the norm over all of them: the sum of its buffers, as in GsAdamTensor. */
 typedef struct {
   const void *grad;               /* [count], aligned to its elements                                      */
-  void *out;                      /* gs_clip_grads only: [count], same type; may be grad                   */
+  void *out;                      /* gs_clip_grads only: [count], same type; may be grad, but no other
+                                     gradient's out or buffer                                              */
   int64_t count;
   int32_t dtype;                  /* GsType                                                                */
   const void *const *more_grads;  /* HOST array of num_more_grads DEVICE pointers, or NULL                 */

@@ -783,6 +783,36 @@ bool rows_shifted(const void *out, int64_t ld_out, const void *in, int64_t ld_in
 // A matrix that moves by TMA.
 bool matrix_bad(const void *p, int64_t ld, int32_t cols) { return bad_ptr(p) || ld < cols || (ld & 7) || ld >= ((int64_t)1 << 38); }
 
+// Whether a gradient's output is also another one's, or another one's buffer.  A table of the outputs with twice as many places as there are at most:
+// a list of 61 costs well below a microsecond.
+bool outputs_shared(const GsGradTensor *tensors, int32_t num_tensors) {
+  constexpr uint32_t kPlaces = 2 * GS_GRAD_MAX_TENSORS;
+  static_assert((kPlaces & (kPlaces - 1)) == 0, "places are masked");
+  int16_t owner[kPlaces];                          // index of the gradient, or -1
+  memset(owner, 0xff, sizeof owner);
+  // the place of the address, or the free one where it would be
+  auto place = [&](const void *p) {
+    uint32_t h = (uint32_t)(((reinterpret_cast<uintptr_t>(p) >> 1) * 0x9e3779b97f4a7c15ull) >> 40) & (kPlaces - 1);
+    while (owner[h] >= 0 && tensors[owner[h]].out != p) h = (h + 1) & (kPlaces - 1);
+    return h;
+  };
+  for (int i = 0; i < num_tensors; ++i) {
+    if (tensors[i].count == 0) continue;
+    const uint32_t h = place(tensors[i].out);
+    if (owner[h] >= 0) return true;
+    owner[h] = (int16_t)i;
+  }
+  for (int i = 0; i < num_tensors; ++i) {
+    const GsGradTensor &t = tensors[i];
+    if (t.count == 0) continue;
+    for (int k = -1; k < t.num_more_grads; ++k) {
+      const int16_t o = owner[place(k < 0 ? t.grad : t.more_grads[k])];
+      if (o >= 0 && o != i) return true;
+    }
+  }
+  return false;
+}
+
 GsStatus grads_ok(GsContext *ctx, const GsGradTensor *tensors, int32_t num_tensors, bool scale, float max_norm, const float *clip, const void *workspace,
                   size_t workspace_bytes) {
   if (num_tensors < 0 || num_tensors > GS_GRAD_MAX_TENSORS || (num_tensors > 0 && !tensors))
@@ -804,6 +834,7 @@ GsStatus grads_ok(GsContext *ctx, const GsGradTensor *tensors, int32_t num_tenso
     more += t.num_more_grads;
     chunks += (t.count >> 13) + 1;
   }
+  if (scale && outputs_shared(tensors, num_tensors)) return fail(ctx, GS_ERR_INVALID_ARG, "a gradient's out is another one's out or buffer");
   if (more > GS_GRAD_MAX_BUFFERS) return fail(ctx, GS_ERR_INVALID_ARG, "more than 1024 further gradient buffers");
   if (chunks >= ((int64_t)1 << 31)) return fail(ctx, GS_ERR_CAPACITY, "the gradients have 2^44 elements or more");
   if (bad_ptr(workspace)) return fail(ctx, GS_ERR_INVALID_ARG, "workspace is NULL or misaligned");
