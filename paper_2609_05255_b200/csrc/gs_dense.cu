@@ -406,8 +406,11 @@ __global__ void __launch_bounds__((kRowsThreads<kForward, kRowsParts<kForward, k
       for (int c = 0; c < chunks; ++c, at.next(a.out_slots)) {
         const uint32_t s = at.s;
         if ((int)(s & 1u) != group) {
-          if (follow && tid == 0 && tma::wait(bar(bars.acc_full[buf]), acc_use(tile) & 1u, dead)) {
-            if (kPair) pair::arrive_first(bar(bars.acc_empty[buf])); else tma::arrive(bar(bars.acc_empty[buf]));
+          if (follow) {
+            if (tid == 0 && tma::wait(bar(bars.acc_full[buf]), acc_use(tile) & 1u, dead)) {
+              if (kPair) pair::arrive_first(bar(bars.acc_empty[buf])); else tma::arrive(bar(bars.acc_empty[buf]));
+            }
+            __syncwarp();
           }
           continue;
         }
