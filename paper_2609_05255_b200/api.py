@@ -761,7 +761,7 @@ class GradList:
             for x in [t.grad, *t.more_grads] + ([t.out] if t.out is not None else []):
                 if x.dtype is not t.grad.dtype or x.numel() != t.grad.numel() or x.device != self.device or not x.is_contiguous() or not x.is_cuda:
                     _invalid("the buffers of a gradient must be contiguous CUDA tensors of one type, size and device")
-                self._memory.append(x.detach())   # a tensor of its own: x may be given other memory
+                self._memory.append(x.untyped_storage())   # (x itself may be given other memory)
             more = (_vp * max(1, len(t.more_grads)))(*[g.data_ptr() for g in t.more_grads])
             self._more.append(more)
             s.grad, s.out, s.count, s.dtype = t.grad.data_ptr(), t.out.data_ptr() if t.out is not None else None, t.grad.numel(), _TYPES[t.grad.dtype]
