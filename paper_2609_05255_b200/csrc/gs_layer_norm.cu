@@ -8,7 +8,7 @@
 // loaded in; the variance is taken about the mean in a second pass over the registers, which loses nothing where the mean is
 // large against the spread.  All sums in fp32, two operations an instruction (add2 and the like): with one each the arithmetic
 // was the bound (1M rows of 256 took 349 us forward, 432 backward; together with the row fetched ahead, the exchanges
-// written out and running pointers 179 and 276, 88 and 85 % of the copy rate).  The grid is persistent: a lane keeps its columns from row to row, so
+// written out and running pointers 176 and 269, 90 and 88 % of the copy rate).  The grid is persistent: a lane keeps its columns from row to row, so
 // gamma and beta stay in registers, and in the backward so do its sums for dgamma and dbeta, which leave as one row of partial
 // sums per CTA and are added up by k_layer_norm_sums in a fixed order (no atomics: the same bits from run to run).
 #include <cuda_bf16.h>
@@ -25,7 +25,9 @@ constexpr int kNormThreads = 256;
 constexpr int kNormPartialRows = 960;     // most CTAs of the backward
 
 // CTAs per SM, of as many registers as the elements of a lane need, and no more CTAs than are resident: 1M rows of 256 in bf16
-// forward 189 us with three, 221 with four (spills), 308 with two; backward in fp16 282 with two, 324 with the compiler's choice.
+// forward 189 us with three, 221 with four (spills), 308 with two; backward in fp16 282 with two, 324 with the compiler's choice.  (Some
+// layouts spill at these counts: aligned ones up to 216 bytes a thread forward and 84 backward, both in fp32, unaligned ones of 32 elements
+// a thread 252 and 128.)
 __host__ __device__ constexpr int fwd_ctas(int elements) { return elements <= 4 ? 6 : elements <= 8 ? 4 : elements <= 16 ? 3 : 2; }
 __host__ __device__ constexpr int bwd_ctas(int elements) { return elements <= 4 ? 4 : elements <= 8 ? 3 : elements <= 16 ? 2 : 1; }
 
